@@ -15,6 +15,7 @@ import os
 import torch  # noqa: F401  (must precede the library: shared HIP runtime)
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfsdp_bucket.so")
+BLOCK_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfsdp_block.so")
 
 c_status = ctypes.c_int32
 c_plan_p = ctypes.c_void_p
@@ -126,3 +127,19 @@ def caller(plan_handle: int, world_size: int, chunk_elems: int, dims: list):
         _caller_type = Caller
         _addresses = tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (*HOT_CALLS, "fsdp_plan_param"))
     return _caller_type(plan_handle, world_size, chunk_elems, dims, _addresses)
+
+
+def load_block():
+    """The block operators' marshaller (csrc/block_marshal.cpp), which links
+    ``libfsdp_block.so`` beside it."""
+    load()
+    try:
+        from . import _block_marshal
+    except ImportError as e:
+        raise ImportError(f"the block operators do not load ({e}): run "
+                          "`python -m paper_2411_00284_amd.build` first; there is no fallback path") from e
+    runtimes = _hip_runtimes_mapped()
+    if len(runtimes) > 1:
+        raise ImportError(f"two HIP runtimes are mapped ({sorted(runtimes)}); "
+                          "import torch before loading libfsdp_block.so")
+    return _block_marshal

@@ -52,10 +52,11 @@ def _dtype_name(t: torch.Tensor) -> str:
 class FsdpError(RuntimeError):
     """A non-zero status from the library."""
 
-    def __init__(self, status: int, where: str):
+    def __init__(self, status: int, where: str, detail: str | None = None):
         lib = _native.load()
         msg = lib.fsdp_status_str(status).decode()
-        detail = lib.fsdp_last_error().decode()
+        if detail is None:
+            detail = lib.fsdp_last_error().decode()
         super().__init__(f"{where}: {msg}" + (f" ({detail})" if detail else ""))
         self.status = status
 

@@ -19,6 +19,7 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -32,6 +33,11 @@ LIB_PATH = os.path.join(PKG, LIB_NAME)
 PROBES_PATH = os.path.join(PKG, "libfsdp_probes.so")
 MARSHAL_PATH = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
+# The block operators: a library of their own, and its marshaller beside it.
+BLOCK_LIB_NAME = "libfsdp_block.so"
+BLOCK_LIB_PATH = os.path.join(PKG, BLOCK_LIB_NAME)
+BLOCK_MARSHAL_PATH = os.path.join(PKG, "_block_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
@@ -43,6 +49,10 @@ DEVICE_FLAGS = [
     "-Wall", "-Wno-unused-command-line-argument",
 ]
 HOST_SOURCES = ["plan.cpp", "auto_wrap.cpp"]
+# The block operators' sums may contract a multiply and an add into one rounding.
+BLOCK_FLAGS = [f if f != "-ffp-contract=off" else "-ffp-contract=fast" for f in DEVICE_FLAGS]
+BLOCK_SOURCES = ["block_norm.hip", "block_linear.hip", "block_distill.hip"]
+BLOCK_HOST_SOURCES = ["block_host.cpp"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-ffp-contract=off", "-D__HIP_PLATFORM_AMD__"]
 
 
@@ -78,6 +88,7 @@ def build(verbose: bool = False, defines=(), out_dir: str | None = None) -> str:
     if variant:
         return lib_path
     _build_marshal(verbose)
+    build_block(verbose)
     pobj = os.path.join(BUILD, "ceiling_probes.o")
     _run([HIPCC, *DEVICE_FLAGS, *inc, "-c", os.path.join(CSRC, "ceiling_probes.hip"), "-o", pobj], verbose)
     tmp = PROBES_PATH + f".tmp{os.getpid()}"
@@ -86,20 +97,49 @@ def build(verbose: bool = False, defines=(), out_dir: str | None = None) -> str:
     return LIB_PATH
 
 
+def build_block(verbose: bool = False, out_dir: str | None = None) -> str:
+    """Compile the block operators' library; returns its path.  With
+    ``out_dir``, the library alone, into that folder."""
+    bdir = os.path.join(out_dir, "_build") if out_dir else BUILD
+    lib_path = os.path.join(out_dir, BLOCK_LIB_NAME) if out_dir else BLOCK_LIB_PATH
+    os.makedirs(bdir, exist_ok=True)
+    inc = [f"-I{INCLUDE}", f"-I{CSRC}", f"-I{os.path.join(ROCM, 'include')}"]
+
+    def compile_one(src):
+        obj = os.path.join(bdir, os.path.splitext(src)[0] + ".o")
+        head = ["g++", *HOST_FLAGS] if src in BLOCK_HOST_SOURCES else [HIPCC, *BLOCK_FLAGS]
+        _run([*head, *inc, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+        return obj
+
+    with ThreadPoolExecutor(4) as pool:
+        objs = list(pool.map(compile_one, [*BLOCK_SOURCES, *BLOCK_HOST_SOURCES]))
+    tmp = lib_path + f".tmp{os.getpid()}"
+    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", f"-Wl,-soname,{BLOCK_LIB_NAME}", "-o", tmp, *objs], verbose)
+    os.replace(tmp, lib_path)
+    if out_dir is None:
+        _build_extension("block_marshal.cpp", BLOCK_MARSHAL_PATH, verbose,
+                         [f"-L{PKG}", "-lfsdp_block", "-Wl,-rpath,$ORIGIN"])
+    return lib_path
+
+
 def _build_marshal(verbose: bool) -> None:
     """The binding's argument marshalling: a CPython extension against torch's
     headers (host code; the bucket library stays free of torch and Python)."""
+    _build_extension("marshal.cpp", MARSHAL_PATH, verbose)
+
+
+def _build_extension(src: str, path: str, verbose: bool, more=()) -> None:
     import torch
     troot = os.path.dirname(torch.__file__)
     abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
     inc = [f"-I{INCLUDE}", f"-I{os.path.join(ROCM, 'include')}", f"-I{sysconfig.get_paths()['include']}",
            f"-isystem{os.path.join(troot, 'include')}",
            f"-isystem{os.path.join(troot, 'include', 'torch', 'csrc', 'api', 'include')}"]
-    tmp = MARSHAL_PATH + f".tmp{os.getpid()}"
+    tmp = path + f".tmp{os.getpid()}"
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
-          f"-D_GLIBCXX_USE_CXX11_ABI={abi}", *inc, os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
-          f"-L{os.path.join(troot, 'lib')}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"], verbose)
-    os.replace(tmp, MARSHAL_PATH)
+          f"-D_GLIBCXX_USE_CXX11_ABI={abi}", *inc, os.path.join(CSRC, src), "-o", tmp,
+          f"-L{os.path.join(troot, 'lib')}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", *more], verbose)
+    os.replace(tmp, path)
 
 
 def clean() -> None:
