@@ -1,11 +1,16 @@
 // The matrix product with bias, activation, factor and residual in its
 // epilogue, and its gradient (include/fsdp_block.h).
 //
-// All three products (x W^T, dz W, dz^T x) are out[i][j] = sum_k A[i][k] B[j][k]
-// with A and B row-major in i / j ("rows") or in k ("columns").
+// A product takes one of these forms:
+//   * product_kernel (block_product.h): 16-bit operands on the 16-byte grid, in
+//     tiles of 256 x 256, 128 x 128 or 64 x 128.  Operands off the grid are
+//     laid on it by a copy into the workspace first.
+//   * row_kernel: at most four rows of x, 16-bit or fp32, at any address.
+//   * product_f32_kernel: fp32, at any address.
+// With few tiles the sum over k is cut into parts, which join_parts_kernel joins
+// in order.
 
-#include "block_device.h"
-#include "block_host.h"
+#include "block_product.h"
 #include "block_join.h"
 
 #include <algorithm>
@@ -13,185 +18,185 @@
 namespace fsdp_block {
 namespace {
 
-// ------------------------------------------------------------------ elementwise
+// ------------------------------------------------------------------ fp32
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
-
-// act(z); 1 + tanh(u) is 2 sigmoid(2u).
-__device__ __forceinline__ float act_value(float z, int act) {
-    switch (act) {
-        case FSDP_ACT_RELU: return z != z ? z : fmaxf(z, 0.f);
-        case FSDP_ACT_SILU: return z * sigmoid(z);
-        case FSDP_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
-        case FSDP_ACT_GELU_TANH: return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
-        default: return z;
-    }
-}
-
-__device__ __forceinline__ float act_slope(float z, int act) {
-    switch (act) {
-        case FSDP_ACT_RELU: return z != z ? z : z > 0.f ? 1.f : 0.f;
-        case FSDP_ACT_SILU: {
-            const float q = sigmoid(z);
-            return q * (1.f + z * (1.f - q));
-        }
-        case FSDP_ACT_GELU:
-            return 0.5f * erfcf(-0.70710678118654752f * z) + z * (0.39894228040143268f * expf(-0.5f * z * z));
-        case FSDP_ACT_GELU_TANH: {
-            const float q = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
-            return q + z * (q * (1.f - q)) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
-        }
-        default: return 1.f;
-    }
-}
-
-// ------------------------------------------------------------------ epilogue
-
-struct Epilogue {
-    const void *bias, *times, *residual;
-    void *pre, *out;
-    int64_t times_stride, residual_stride, pre_stride, out_stride;
-    int act;
+// A kTile x kTile tile of out in four waves, from operands of any alignment.
+// The fp32 matrix instructions run at a sixteenth of the bf16 rate, so the rest
+// needs no care: registers hold the next step while one is worked on in LDS.
+// A step is two 16-byte units of both operands per thread.
+template <int kTile>
+struct Step32 {
+    static constexpr int kDeep = 512 * 4 / kTile;      // k of a step: 16 or 32
+    static constexpr int kRow = kDeep + 4;             // floats of a row in LDS, padded by 16 bytes
 };
 
-// z -> out at row i, column j; `z` is the product, without the bias.
-template <typename T>
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t i, int64_t j, float z) {
-    if (e.bias) z += float(static_cast<const T*>(e.bias)[j]);
-    if (e.pre) static_cast<T*>(e.pre)[i * e.pre_stride + j] = T(z);
-    z = act_value(z, e.act);
-    if (e.times) z *= float(static_cast<const T*>(e.times)[i * e.times_stride + j]);
-    if (e.residual) z += float(static_cast<const T*>(e.residual)[i * e.residual_stride + j]);
-    static_cast<T*>(e.out)[i * e.out_stride + j] = T(z);
-}
-
-// ------------------------------------------------------------------ product
-
-struct Product {
-    const void *a, *b;
-    int64_t a_stride, b_stride;
-    int64_t m, n, k;                 // out [m, n]
-    Epilogue e;
-};
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16 f16x8 __attribute__((ext_vector_type(8)));
-
-// 16 bytes of A rows and of B rows per lane -> a 16 x 16 tile.  Lane l holds
-// row l % 16 of both and the (l / 16)-th 16 bytes of a 64-byte run of k; the
-// tile's element r of lane l is at A row 4 (l / 16) + r, B row l % 16.
-__device__ __forceinline__ f32x4 mma(Eight<bf16> a, Eight<bf16> b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(Eight<f16> a, Eight<f16> b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
-}
-
-// The 16 bytes that a load and a lane of a matrix instruction take.
-template <typename T>
-struct Unit {
-    static constexpr int n = 16 / int(sizeof(T));
-    typedef T type __attribute__((ext_vector_type(n)));
-    struct __attribute__((packed, aligned(sizeof(T)))) any {
-        type v;
+// kColumns: the operand lies k-major, a unit is four rows at one k.
+template <int kTile, bool kColumns>
+__device__ __forceinline__ void load_f32(const float* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k1,
+                                         f32x4 (&out)[2]) {
+    constexpr int kDeep = Step32<kTile>::kDeep, kAcross = kColumns ? kTile / 4 : kDeep / 4;
+    struct __attribute__((packed, aligned(4))) any {
+        f32x4 v;
     };
-};
-
-// A 128 x 128 tile of out in 256 threads, from operands of any alignment,
-// stride and size: the form for what the aligned one does not take.
-constexpr int kAnyTile = 128;
-
-// Loads two units of a 128-row, 64-byte operand tile: of rows first + .., k from
-// k0.  kColumns: the operand lies k-major, a unit is n rows at one k.
-template <typename T, bool kColumns>
-__device__ __forceinline__ void load_any(const T* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k,
-                                         typename Unit<T>::type (&out)[2]) {
-    constexpr int n = Unit<T>::n, kDeep = 4 * n;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int c = int(threadIdx.x) + 256 * u;
-        const int64_t i = first + (kColumns ? c % (kAnyTile / n) * n : c / 4);
-        const int64_t j = k0 + (kColumns ? c / (kAnyTile / n) : c % 4 * n);
-        static_assert(kAnyTile / n * kDeep == 512, "two units per thread");
-        const int64_t left = kColumns ? (j < k ? rows - i : 0) : (i < rows ? k - j : 0);
-        const T* at = kColumns ? p + j * stride + i : p + i * stride + j;
-        if (left >= n) {
-            out[u] = reinterpret_cast<const typename Unit<T>::any*>(at)->v;
+        const int64_t i = first + (kColumns ? c % kAcross * 4 : c / kAcross);
+        const int64_t j = k0 + (kColumns ? c / kAcross : c % kAcross * 4);
+        const int64_t left = kColumns ? (j < k1 ? rows - i : 0) : (i < rows ? k1 - j : 0);
+        const float* at = kColumns ? p + j * stride + i : p + i * stride + j;
+        if (left >= 4) {
+            out[u] = reinterpret_cast<const any*>(at)->v;
         } else {
 #pragma unroll
-            for (int e = 0; e < n; ++e) out[u][e] = e < left ? at[e] : T(0.f);
+            for (int e = 0; e < 4; ++e) out[u][e] = e < left ? at[e] : 0.f;
         }
     }
 }
 
-template <typename T>
-using AnyTile = T[kAnyTile][5 * Unit<T>::n];     // rows of 64 bytes of k, padded by 16
-
-template <typename T, bool kColumns>
-__device__ __forceinline__ void keep_any(AnyTile<T>& tile, const typename Unit<T>::type (&in)[2]) {
-    constexpr int n = Unit<T>::n;
+template <int kTile, bool kColumns>
+__device__ __forceinline__ void keep_f32(float* tile, const f32x4 (&in)[2]) {
+    constexpr int kRow = Step32<kTile>::kRow, kAcross = kColumns ? kTile / 4 : Step32<kTile>::kDeep / 4;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int c = int(threadIdx.x) + 256 * u;
         if constexpr (kColumns) {
 #pragma unroll
-            for (int e = 0; e < n; ++e) tile[c % (kAnyTile / n) * n + e][c / (kAnyTile / n)] = in[u][e];
+            for (int e = 0; e < 4; ++e) tile[(c % kAcross * 4 + e) * kRow + c / kAcross] = in[u][e];
         } else {
-            *reinterpret_cast<typename Unit<T>::type*>(&tile[c / 4][c % 4 * n]) = in[u];
+            *reinterpret_cast<f32x4*>(tile + c / kAcross * kRow + c % kAcross * 4) = in[u];
         }
     }
 }
 
-template <typename T, bool kColumnsA, bool kColumnsB>
-__global__ __launch_bounds__(256) void product_any_kernel(const Product p) {
-    constexpr int n = Unit<T>::n, kDeep = 4 * n;
-    using U = typename Unit<T>::type;
-    __shared__ __attribute__((aligned(16))) AnyTile<T> ta, tb;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wi = wave / 2 * 64, wj = wave % 2 * 64;
-    const int64_t tiles_n = (p.n + kAnyTile - 1) / kAnyTile;
-    const int64_t i0 = blockIdx.x / tiles_n * kAnyTile, j0 = blockIdx.x % tiles_n * kAnyTile;
-    const T* a = static_cast<const T*>(p.a);
-    const T* b = static_cast<const T*>(p.b);
-    f32x4 acc[4][4] = {};            // [A tile][B tile]
-    U ra[2], rb[2];
-    load_any<T, kColumnsA>(a, p.a_stride, i0, p.m, 0, p.k, ra);
-    load_any<T, kColumnsB>(b, p.b_stride, j0, p.n, 0, p.k, rb);
-    for (int64_t k = 0; k < p.k; k += kDeep) {
+template <int kTile, bool kColumnsA, bool kColumnsB>
+__global__ __launch_bounds__(256) void product_f32_kernel(const Product p) {
+    constexpr int kDeep = Step32<kTile>::kDeep, kRow = Step32<kTile>::kRow, kN = kTile / 32;    // 16-row tiles of a wave
+    __shared__ __attribute__((aligned(16))) float ta[kTile * kRow], tb[kTile * kRow];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % 16, q = lane / 16;
+    const int wi = wave / 2 * (kTile / 2), wj = wave % 2 * (kTile / 2);
+    const TilePlace t = tile_place(blockIdx.x, unsigned((p.m + kTile - 1) / kTile), unsigned((p.n + kTile - 1) / kTile),
+                                   unsigned(p.count));
+    const int64_t i0 = int64_t(t.row) * kTile, j0 = int64_t(t.column) * kTile;
+    const int64_t k0 = t.part * p.part_k, k1 = min(k0 + p.part_k, p.k);
+    const float* a = static_cast<const float*>(p.a);
+    const float* b = static_cast<const float*>(p.b);
+    f32x4 acc[kN][kN] = {};          // [A tile][B tile]
+    f32x4 ra[2], rb[2];
+    load_f32<kTile, kColumnsA>(a, p.a_stride, i0, p.m, k0, k1, ra);
+    load_f32<kTile, kColumnsB>(b, p.b_stride, j0, p.n, k0, k1, rb);
+    for (int64_t k = k0; k < k1; k += kDeep) {
         __syncthreads();
-        keep_any<T, kColumnsA>(ta, ra);
-        keep_any<T, kColumnsB>(tb, rb);
+        keep_f32<kTile, kColumnsA>(ta, ra);
+        keep_f32<kTile, kColumnsB>(tb, rb);
         __syncthreads();
-        if (k + kDeep < p.k) {
-            load_any<T, kColumnsA>(a, p.a_stride, i0, p.m, k + kDeep, p.k, ra);
-            load_any<T, kColumnsB>(b, p.b_stride, j0, p.n, k + kDeep, p.k, rb);
-        }
-        U fa[4], fb[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            fa[x] = *reinterpret_cast<const U*>(&ta[wi + 16 * x + lane % 16][lane / 16 * n]);
-            fb[x] = *reinterpret_cast<const U*>(&tb[wj + 16 * x + lane % 16][lane / 16 * n]);
+        if (k + kDeep < k1) {
+            load_f32<kTile, kColumnsA>(a, p.a_stride, i0, p.m, k + kDeep, k1, ra);
+            load_f32<kTile, kColumnsB>(b, p.b_stride, j0, p.n, k + kDeep, k1, rb);
         }
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int s = 0; s < kDeep / 16; ++s) {
+            f32x4 fa[kN], fb[kN];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) acc[x][y] = mma(fa[x], fb[y], acc[x][y]);
+            for (int x = 0; x < kN; ++x) {
+                fa[x] = *reinterpret_cast<const f32x4*>(ta + (wi + 16 * x + r) * kRow + 16 * s + q * 4);
+                // Rows of B tiles are dealt so that a lane ends with eight neighbouring columns of two tiles.
+                fb[x] = *reinterpret_cast<const f32x4*>(tb + (wj + x / 2 * 32 + r / 4 * 8 + x % 2 * 4 + r % 4) * kRow + 16 * s + q * 4);
+            }
+#pragma unroll
+            for (int x = 0; x < kN; ++x)
+#pragma unroll
+                for (int y = 0; y < kN; ++y) acc[x][y] = mma(fb[y], fa[x], acc[x][y]);
+        }
     }
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < kN; ++x)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int y = 0; y < kN; y += 2) {
+            float z[8];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t i = i0 + wi + 16 * x + lane / 16 * 4 + r, j = j0 + wj + 16 * y + lane % 16;
-                if (i < p.m && j < p.n) finish<T>(p.e, i, j, acc[x][y][r]);
-            }
+            for (int c = 0; c < 8; ++c) z[c] = acc[x][y + c / 4][c % 4];
+            leave8<float, kColumnsB>(p, t.part, i0 + wi + 16 * x + r, j0 + wj + y / 2 * 32 + q * 8, z);
+        }
+}
+
+// ------------------------------------------------------------------ few rows
+
+// x W^T of at most kRows rows of x: a wave takes kOut rows of W, eight elements
+// per lane at a time, and reads W once; x comes from cache.  Bound by reading W.
+constexpr int kRowOut = 2;
+
+template <typename T, int kRows>
+__global__ __launch_bounds__(256) void row_kernel(const Product p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t j0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * kRowOut;
+    if (j0 >= p.n) return;
+    const T* w[kRowOut];
+#pragma unroll
+    for (int o = 0; o < kRowOut; ++o) w[o] = static_cast<const T*>(p.b) + min(j0 + o, p.n - 1) * p.b_stride;
+    const T* x = static_cast<const T*>(p.a);
+    float sum[kRowOut][kRows] = {};
+    const auto add = [&](int64_t k, int n) {
+        Eight<T> v[kRowOut];
+#pragma unroll
+        for (int o = 0; o < kRowOut; ++o) v[o] = load_some(w[o] + k, n);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const Eight<T> u = load_some(x + min(int64_t(i), p.m - 1) * p.a_stride + k, n);
+#pragma unroll
+            for (int o = 0; o < kRowOut; ++o)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sum[o][i] += float(v[o][c]) * float(u[c]);
+        }
+    };
+    int64_t k = lane * 8;
+#pragma unroll 4
+    for (; k + 8 <= p.k; k += 512) add(k, 8);
+    if (k < p.k) add(k, int(p.k - k));
+#pragma unroll
+    for (int o = 0; o < kRowOut; ++o)
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) sum[o][i] = wave_sum(sum[o][i]);
+    if (lane < p.m)
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (lane == i)
+#pragma unroll
+                for (int o = 0; o < kRowOut; ++o) {
+                    float z[8] = {sum[o][i]};
+                    if (j0 + o < p.n) finish8<T>(p.e, i, j0 + o, 1, z);
+                }
+}
+
+// ------------------------------------------------------------------ onto the grid
+
+// Copies matrices to rows of whole 16-byte units, zeros after their columns.
+struct PadArgs {
+    const uint16_t* from[2];
+    uint16_t* to[2];
+    int64_t rows[2], cols[2], stride[2], units[2];     // units: of a padded row
+};
+
+__global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    struct __attribute__((packed, aligned(2))) any {
+        u16x8 v;
+    };
+    const int64_t first = a.rows[0] * a.units[0], all = first + a.rows[1] * a.units[1];
+    for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < all; u += int64_t(gridDim.x) * 256) {
+        const int which = u >= first;
+        const int64_t unit = which ? u - first : u, row = unit / a.units[which], j = unit % a.units[which] * 8;
+        const uint16_t* at = a.from[which] + row * a.stride[which] + j;
+        const int64_t left = a.cols[which] - j;
+        u16x8 v;
+        if (left >= 8) {
+            v = reinterpret_cast<const any*>(at)->v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? at[e] : uint16_t(0);
+        }
+        *reinterpret_cast<u16x8*>(a.to[which] + unit * 8) = v;
+    }
 }
 
 // ------------------------------------------------------------------ dz
@@ -234,7 +239,8 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
                 if (a.act != FSDP_ACT_NONE) dz[e] *= act_slope(float(z[e]), a.act);
                 sum[e] += dz[e];
             }
-            if (a.dz) store_some(static_cast<T*>(a.dz) + i * a.dz_stride + j, left, dz);
+            // dz's rows are the workspace's: whole units, zeros after the columns (load_some gave zeros).
+            if (a.dz) store_some(static_cast<T*>(a.dz) + i * a.dz_stride + j, 8, dz);
         }
     if (!a.part) return;
 #pragma unroll
@@ -254,14 +260,170 @@ fsdp_status with_type(fsdp_dtype dtype, F f) {
     return dtype == FSDP_DTYPE_BF16 ? f(bf16(0.f)) : dtype == FSDP_DTYPE_F16 ? f(f16(0.f)) : f(0.f);
 }
 
-// One product.  kColumns*: the operand lies k-major.
+// The forms of a product in tiles.  Times in us of a step of 64 k (fp32: of 32)
+// on one MI355X: `alone` with one workgroup or few on a CU, `full` with every CU
+// holding `held` of them, and `fixed` for the start and the end of a tile, as
+// measured over products from 16 x 14336 x 4096 to 8192 x 28672 x 8192.
+struct Form {
+    int tile_m, tile_n, steps, held;
+    double alone, full, fixed;
+};
+constexpr Form kForms16[] = {
+    {256, 256, 2, 1, 1.15, 1.60, 6.0},
+    {128, 128, 2, 2, 0.60, 0.97, 4.0},
+    {128, 128, 4, 1, 0.36, 0.52, 3.5},
+    {64, 128, 4, 1, 0.25, 0.32, 3.5},
+};
+constexpr Form kForms32[] = {
+    {128, 128, 0, 2, 2.2, 4.0, 5.0},
+    {64, 64, 0, 4, 0.8, 2.0, 4.0},
+};
+
+// How one product is run.
+struct Cut {
+    const Form* form = nullptr;      // NULL: row_kernel
+    int count = 1;                   // parts of k
+    int64_t part_k = 0;
+    // Byte offsets in the workspace and its size: the operands laid on the grid, the parts.
+    int64_t pad_a = -1, pad_b = -1, parts = -1, bytes = 0;
+};
+
+struct Shape {
+    int64_t m, n, k;
+    fsdp_dtype dtype;
+    bool columns_a, columns_b;
+};
+
+constexpr int64_t kMostRows = 4;     // of row_kernel
+
+// The form and the cut with the least expected time: whole rounds of workgroups
+// over the CUs, what is left of the last round, reading the operands at 5.5 TB/s
+// if that takes longer, and the join of the parts (3 us, and 8 bytes moved per
+// value and part).  From at most four rows of x on, row_kernel reads the weight
+// at HBM's rate in one launch.
+Cut choose(const Shape& s, int cus) {
+    Cut best;
+    if (s.m <= kMostRows && !s.columns_a && !s.columns_b) return best;
+    const bool wide = s.dtype == FSDP_DTYPE_F32;
+    const Form* const forms = wide ? kForms32 : kForms16;
+    const int step_k = wide ? 32 : 64;
+    const int64_t steps = std::max<int64_t>(1, ceil_div(s.k, step_k));
+    const double bytes = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k));
+    double least = 0;
+    for (int f = 0; f < (wide ? 2 : 4); ++f) {
+        const Form& form = forms[f];
+        const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n);
+        for (int64_t parts : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (parts > 1 && (steps < 4 * parts || tiles * (parts - 1) > 4 * int64_t(cus))) break;
+            const int64_t each = ceil_div(steps, parts), groups = tiles * ceil_div(steps, each);
+            const int64_t slots = int64_t(cus) * form.held, whole = groups / slots, rest = groups % slots;
+            double time = double(whole) * (double(each) * form.full + form.fixed);
+            if (rest) time += double(each) * std::max(form.alone, form.full * double(rest) / double(slots)) + form.fixed;
+            time = std::max(time, bytes / 5.5e6 + form.fixed);
+            if (parts > 1) time += 3.0 + double(parts) * double(s.m) * double(s.n) * 8 / 5e6;
+            if (!best.form || time < least) {
+                least = time;
+                best.form = &form;
+                best.part_k = each * step_k;
+                best.count = int(ceil_div(steps, each));
+            }
+        }
+    }
+    return best;
+}
+
+struct Operand16 {
+    const void* p;
+    int64_t rows, cols, stride;      // as it lies in memory
+    bool columns;
+    bool zeros;                      // zeros follow a row, up to a whole 16-byte unit
+};
+
+// Whether an operand lies on the 16-byte grid in whole units, as product_kernel
+// reads it, with offsets of 64 rows or of a tile in 31 bits.
+bool on_grid(const Operand16& o) {
+    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % 8 == 0 && o.stride < (1 << 22) && (o.zeros || o.cols % 8 == 0);
+}
+
+// Adds a product's needs to those of `bytes`.
+Cut plan(const Shape& s, const Operand16& a, const Operand16& b, int cus, int64_t bytes) {
+    Cut c = choose(s, cus);
+    c.bytes = bytes;
+    if (!c.form || s.m == 0 || s.n == 0 || s.k == 0) return c;
+    const auto take = [&](int64_t n) {
+        const int64_t at = c.bytes;
+        c.bytes += round_up(n, 256);
+        return at;
+    };
+    if (s.dtype != FSDP_DTYPE_F32) {
+        if (!on_grid(a)) c.pad_a = take(a.rows * round_up(a.cols, 8) * 2);
+        if (!on_grid(b)) c.pad_b = take(b.rows * round_up(b.cols, 8) * 2);
+    }
+    if (c.count > 1) c.parts = take(int64_t(c.count) * s.m * round_up(s.n, 8) * 4);
+    return c;
+}
+
 template <bool kColumnsA, bool kColumnsB>
-fsdp_status product(const Product& p, fsdp_dtype dtype, hipStream_t stream) {
-    if (p.m == 0 || p.n == 0) return FSDP_OK;
-    return with_type(dtype, [&](auto type) {
-        const int64_t tiles = ceil_div(p.m, kAnyTile) * ceil_div(p.n, kAnyTile);
-        return launch(product_any_kernel<decltype(type), kColumnsA, kColumnsB>, p, dim3(unsigned(tiles)), 256, stream);
-    });
+fsdp_status launch_tiles(const Product& p, const Cut& c, fsdp_dtype dtype, hipStream_t stream) {
+    const Form& f = *c.form;
+    const dim3 grid(unsigned(ceil_div(p.m, f.tile_m) * ceil_div(p.n, f.tile_n) * c.count));
+    if (dtype == FSDP_DTYPE_F32)
+        return f.tile_m == 128 ? launch(product_f32_kernel<128, kColumnsA, kColumnsB>, p, grid, 256, stream)
+                               : launch(product_f32_kernel<64, kColumnsA, kColumnsB>, p, grid, 256, stream);
+    const auto of = [&](auto type) {
+        using T = decltype(type);
+        if (f.tile_m == 256) return launch(product_kernel<T, kColumnsA, kColumnsB, 256, 256, 2>, p, grid, 256, stream);
+        if (f.tile_m == 64) return launch(product_kernel<T, kColumnsA, kColumnsB, 64, 128, 4>, p, grid, 256, stream);
+        return f.steps == 2 ? launch(product_kernel<T, kColumnsA, kColumnsB, 128, 128, 2>, p, grid, 256, stream)
+                            : launch(product_kernel<T, kColumnsA, kColumnsB, 128, 128, 4>, p, grid, 256, stream);
+    };
+    return dtype == FSDP_DTYPE_BF16 ? of(bf16(0.f)) : of(f16(0.f));
+}
+
+// One product, as `c` says.
+fsdp_status run_product(const Shape& s, const Operand16& a, const Operand16& b, const Epilogue& e, const Cut& c, char* ws,
+                        hipStream_t stream) {
+    if (s.m == 0 || s.n == 0) return FSDP_OK;
+    Product p{a.p, b.p, a.stride, b.stride, s.m, s.n, s.k, e, nullptr, s.k, 1};
+    if (!c.form) {
+        const dim3 grid(unsigned(ceil_div(s.n, 4 * kRowOut)));
+        return with_type(s.dtype, [&](auto type) {
+            using T = decltype(type);
+            return s.m == 1   ? launch(row_kernel<T, 1>, p, grid, 256, stream)
+                   : s.m == 2 ? launch(row_kernel<T, 2>, p, grid, 256, stream)
+                              : launch(row_kernel<T, 4>, p, grid, 256, stream);
+        });
+    }
+    fsdp_status st;
+    if (c.pad_a >= 0 || c.pad_b >= 0) {
+        PadArgs pad{};
+        const auto lay = [&](int which, const Operand16& o, int64_t at, const void** to, int64_t* stride) {
+            pad.units[which] = 1;
+            if (at < 0) return;
+            pad.from[which] = static_cast<const uint16_t*>(o.p);
+            pad.to[which] = reinterpret_cast<uint16_t*>(ws + at);
+            pad.rows[which] = o.rows;
+            pad.cols[which] = o.cols;
+            pad.stride[which] = o.stride;
+            pad.units[which] = ceil_div(o.cols, 8);
+            *to = ws + at;
+            *stride = pad.units[which] * 8;
+        };
+        lay(0, a, c.pad_a, &p.a, &p.a_stride);
+        lay(1, b, c.pad_b, &p.b, &p.b_stride);
+        const int64_t units = pad.rows[0] * pad.units[0] + pad.rows[1] * pad.units[1];
+        if ((st = launch(pad_kernel, pad, dim3(unsigned(std::min<int64_t>(ceil_div(units, 256), 1 << 16))), 256, stream)) != FSDP_OK)
+            return st;
+    }
+    p.part_k = c.part_k;
+    p.count = c.count;
+    p.parts = c.parts < 0 ? nullptr : reinterpret_cast<float*>(ws + c.parts);
+    st = s.columns_a ? launch_tiles<true, true>(p, c, s.dtype, stream)
+         : s.columns_b ? launch_tiles<false, true>(p, c, s.dtype, stream)
+                       : launch_tiles<false, false>(p, c, s.dtype, stream);
+    if (st != FSDP_OK || c.count == 1) return st;
+    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(s.m * ceil_div(s.n, 8), 256), 1 << 13)));
+    return with_type(s.dtype, [&](auto type) { return launch(join_parts_kernel<decltype(type)>, p, grid, 256, stream); });
 }
 
 fsdp_status check_sizes(int64_t m, int64_t n, int64_t k, fsdp_dtype dtype, fsdp_activation act) {
@@ -271,8 +433,8 @@ fsdp_status check_sizes(int64_t m, int64_t n, int64_t k, fsdp_dtype dtype, fsdp_
     // Row and column counts travel as 32-bit values in the kernels, tiles as a launch's workgroups.
     if (m > INT32_MAX / 2 || n > INT32_MAX / 2 || k > INT32_MAX / 2) return fail(FSDP_ERR_OVERFLOW, "a size is above 2^30");
     const int64_t most = int64_t(1) << 22;
-    if (ceil_div(m, kAnyTile) * ceil_div(n, kAnyTile) > most || ceil_div(m, kAnyTile) * ceil_div(k, kAnyTile) > most ||
-        ceil_div(n, kAnyTile) * ceil_div(k, kAnyTile) > most)
+    if (ceil_div(m, 64) * ceil_div(n, 64) > most || ceil_div(m, 64) * ceil_div(k, 64) > most ||
+        ceil_div(n, 64) * ceil_div(k, 64) > most)
         return fail(FSDP_ERR_OVERFLOW, "a product has too many tiles");
     return FSDP_OK;
 }
@@ -310,28 +472,57 @@ fsdp_status check_grad(const fsdp_linear_grad_args& a) {
     return c.done();
 }
 
+int64_t row_stride(int64_t rows, int64_t cols, int64_t stride) { return rows > 1 ? stride : round_up(cols, 8); }
+
+// The operands of the three products.
+Shape forward_shape(const fsdp_linear_args& a) { return {a.m, a.n, a.k, a.dtype, false, false}; }
+Operand16 forward_x(const fsdp_linear_args& a) { return {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false, false}; }
+Operand16 forward_w(const fsdp_linear_args& a) { return {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false, false}; }
+
 // What a gradient needs besides its outputs.
 struct GradParts {
     bool slopes = false;             // dz is not dout
     int64_t parts = 0, part_rows = 1;            // row parts of dbias
     int64_t dz = -1, dbias = -1;     // byte offsets
-    int64_t bytes = 0;
+    int64_t bytes = 0;               // of the workspace
+    Shape dx_shape, dw_shape;
+    Operand16 dz_rows, weight, dz_columns, x;
+    Cut dx, dw;
 };
 
-GradParts parts_of(const fsdp_linear_grad_args& a, int cus) {
+GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
     GradParts g;
-    if (a.m == 0 || a.n == 0) return g;
     g.slopes = a.times || a.activation != FSDP_ACT_NONE;
-    const int64_t columns = ceil_div(a.n, 512);
-    g.part_rows = std::max<int64_t>(4, round_up(ceil_div(a.m * columns, 8 * int64_t(cus)), 4));
-    g.parts = ceil_div(a.m, g.part_rows);
-    if (g.slopes && (a.dx || a.dweight)) {
-        g.dz = g.bytes;
-        g.bytes += round_up(a.m * round_up(a.n, 8) * elem_bytes(a.dtype), 256);
+    if (a.m > 0 && a.n > 0) {
+        const int64_t columns = ceil_div(a.n, 512);
+        g.part_rows = std::max<int64_t>(4, round_up(ceil_div(a.m * columns, 8 * int64_t(cus)), 4));
+        g.parts = ceil_div(a.m, g.part_rows);
+        if (g.slopes && (a.dx || a.dweight)) {
+            g.dz = g.bytes;
+            g.bytes += round_up(a.m * round_up(a.n, 8) * elem_bytes(a.dtype), 256);
+        }
+        if (a.dbias) {
+            g.dbias = g.bytes;
+            g.bytes += round_up(g.parts * a.n * 4, 256);
+        }
     }
-    if (a.dbias) {
-        g.dbias = g.bytes;
-        g.bytes += round_up(g.parts * a.n * 4, 256);
+    const void* const dz = g.dz >= 0 ? ws + g.dz : a.dout;
+    const int64_t stride = g.dz >= 0 ? round_up(a.n, 8) : row_stride(a.m, a.n, a.dout_stride);
+    g.dz_rows = {dz, a.m, a.n, stride, false, g.dz >= 0};
+    g.dz_columns = {dz, a.m, a.n, stride, true, g.dz >= 0};
+    g.weight = {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), true, false};
+    g.x = {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), true, false};
+    g.dx_shape = {a.m, a.k, a.n, a.dtype, false, true};
+    g.dw_shape = {a.n, a.k, a.m, a.dtype, true, true};
+    const int64_t own = g.bytes;
+    // The two products follow each other on the stream: they share what they need.
+    if (a.dx) {
+        g.dx = plan(g.dx_shape, g.dz_rows, g.weight, cus, own);
+        g.bytes = std::max(g.bytes, g.dx.bytes);
+    }
+    if (a.dweight) {
+        g.dw = plan(g.dw_shape, g.dz_columns, g.x, cus, own);
+        g.bytes = std::max(g.bytes, g.dw.bytes);
     }
     return g;
 }
@@ -344,9 +535,11 @@ using namespace fsdp_block;
 extern "C" fsdp_status fsdp_block_linear_workspace(const fsdp_linear_args* args, int64_t* bytes) {
     clear_error();
     if (!args || !bytes) return fail(FSDP_ERR_INVALID, "args or bytes is NULL");
-    const fsdp_status st = check_linear(*args);
+    fsdp_status st = check_linear(*args);
     if (st != FSDP_OK) return st;
-    *bytes = 0;
+    const int cus = cu_count(&st);
+    if (cus == 0) return st;
+    *bytes = plan(forward_shape(*args), forward_x(*args), forward_w(*args), cus, 0).bytes;
     return FSDP_OK;
 }
 
@@ -355,12 +548,17 @@ extern "C" fsdp_status fsdp_block_linear(const fsdp_linear_args* args, void* wor
     clear_error();
     if (!args) return fail(FSDP_ERR_INVALID, "args is NULL");
     const fsdp_linear_args& a = *args;
-    const fsdp_status st = check_linear(a);
+    fsdp_status st = check_linear(a);
     if (st != FSDP_OK) return st;
-    const Product p{a.x, a.weight, a.x_stride, a.weight_stride, a.m, a.n, a.k,
-                    {a.bias, a.times, a.residual, a.pre, a.out, a.times_stride, a.residual_stride, a.pre_stride,
-                     a.out_stride, a.activation}};
-    return product<false, false>(p, a.dtype, stream);
+    const int cus = cu_count(&st);
+    if (cus == 0) return st;
+    const Shape s = forward_shape(a);
+    const Operand16 x = forward_x(a), w = forward_w(a);
+    const Cut c = plan(s, x, w, cus, 0);
+    if ((st = check_workspace(workspace, workspace_bytes, c.bytes)) != FSDP_OK) return st;
+    const Epilogue e{a.bias, a.times, a.residual, a.pre, a.out, a.times_stride, a.residual_stride, a.pre_stride, a.out_stride,
+                     a.activation};
+    return run_product(s, x, w, e, c, static_cast<char*>(workspace), stream);
 }
 
 extern "C" fsdp_status fsdp_block_linear_grad_workspace(const fsdp_linear_grad_args* args, int64_t* bytes) {
@@ -370,7 +568,7 @@ extern "C" fsdp_status fsdp_block_linear_grad_workspace(const fsdp_linear_grad_a
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
-    *bytes = parts_of(*args, cus).bytes;
+    *bytes = parts_of(*args, cus, nullptr).bytes;
     return FSDP_OK;
 }
 
@@ -383,19 +581,13 @@ extern "C" fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args,
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
-    const GradParts g = parts_of(a, cus);
-    if ((st = check_workspace(workspace, workspace_bytes, g.bytes)) != FSDP_OK) return st;
     char* const ws = static_cast<char*>(workspace);
-    const void* dz = a.dout;
-    int64_t dz_stride = a.dout_stride;
-    if (g.dz >= 0) {
-        dz = ws + g.dz;
-        dz_stride = round_up(a.n, 8);
-    }
+    const GradParts g = parts_of(a, cus, ws);
+    if ((st = check_workspace(workspace, workspace_bytes, g.bytes)) != FSDP_OK) return st;
     float* const part = g.dbias < 0 ? nullptr : reinterpret_cast<float*>(ws + g.dbias);
     if (a.m > 0 && a.n > 0 && (g.dz >= 0 || part || a.dtimes)) {
         const SlopeArgs s{a.dout, a.pre, a.times, g.dz >= 0 ? ws + g.dz : nullptr, a.dtimes, part, a.dout_stride,
-                          a.pre_stride, a.times_stride, dz_stride, a.dtimes_stride, a.m, a.n, g.part_rows, a.activation};
+                          a.pre_stride, a.times_stride, g.dz_rows.stride, a.dtimes_stride, a.m, a.n, g.part_rows, a.activation};
         const dim3 grid(unsigned(ceil_div(a.n, 512)), unsigned(g.parts));
         st = with_type(a.dtype, [&](auto type) { return launch(slope_kernel<decltype(type)>, s, grid, 256, stream); });
         if (st != FSDP_OK) return st;
@@ -403,15 +595,13 @@ extern "C" fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args,
     Join j(int(a.n));
     j.add(a.dbias, part, g.parts, a.dbias ? 1 : 0, a.dtype);
     if ((st = j.run(a.dtype, stream)) != FSDP_OK) return st;
+    const auto plain = [](void* out, int64_t stride) {
+        return Epilogue{nullptr, nullptr, nullptr, nullptr, out, 0, 0, 0, stride, FSDP_ACT_NONE};
+    };
     if (a.dx) {
-        const Product p{dz, a.weight, dz_stride, a.weight_stride, a.m, a.k, a.n,
-                        {nullptr, nullptr, nullptr, nullptr, a.dx, 0, 0, 0, a.dx_stride, FSDP_ACT_NONE}};
-        if ((st = product<false, true>(p, a.dtype, stream)) != FSDP_OK) return st;
+        st = run_product(g.dx_shape, g.dz_rows, g.weight, plain(a.dx, a.dx_stride), g.dx, ws, stream);
+        if (st != FSDP_OK) return st;
     }
-    if (a.dweight) {
-        const Product p{dz, a.x, dz_stride, a.x_stride, a.n, a.k, a.m,
-                        {nullptr, nullptr, nullptr, nullptr, a.dweight, 0, 0, 0, a.dweight_stride, FSDP_ACT_NONE}};
-        st = product<true, true>(p, a.dtype, stream);
-    }
+    if (a.dweight) st = run_product(g.dw_shape, g.dz_columns, g.x, plain(a.dweight, a.dweight_stride), g.dw, ws, stream);
     return st;
 }

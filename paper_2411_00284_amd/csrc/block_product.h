@@ -1,0 +1,413 @@
+// The matrix product of 16-bit operands on the 16-byte grid, its epilogue, and
+// what else the product kernels share.
+//
+// All products of a linear layer (x W^T, dz W, dz^T x) are
+// out[i][j] = sum_k A[i][k] B[j][k]; an operand lies row by row (k contiguous:
+// "rows") or k by k (i or j contiguous: "columns").
+#pragma once
+
+#include "block_device.h"
+#include "block_host.h"
+
+namespace fsdp_block {
+namespace {
+
+// ------------------------------------------------------------------ elementwise
+
+__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+
+// act(z); 1 + tanh(u) is 2 sigmoid(2u).
+__device__ __forceinline__ float act_value(float z, int act) {
+    switch (act) {
+        case FSDP_ACT_RELU: return z != z ? z : fmaxf(z, 0.f);
+        case FSDP_ACT_SILU: return z * sigmoid(z);
+        case FSDP_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
+        case FSDP_ACT_GELU_TANH: return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
+        default: return z;
+    }
+}
+
+__device__ __forceinline__ float act_slope(float z, int act) {
+    switch (act) {
+        case FSDP_ACT_RELU: return z != z ? z : z > 0.f ? 1.f : 0.f;
+        case FSDP_ACT_SILU: {
+            const float q = sigmoid(z);
+            return q * (1.f + z * (1.f - q));
+        }
+        case FSDP_ACT_GELU:
+            return 0.5f * erfcf(-0.70710678118654752f * z) + z * (0.39894228040143268f * expf(-0.5f * z * z));
+        case FSDP_ACT_GELU_TANH: {
+            const float q = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
+            return q + z * (q * (1.f - q)) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
+        }
+        default: return 1.f;
+    }
+}
+
+// ------------------------------------------------------------------ arguments
+
+struct Epilogue {
+    const void *bias, *times, *residual;
+    void *pre, *out;
+    int64_t times_stride, residual_stride, pre_stride, out_stride;
+    int act;
+};
+
+struct Product {
+    const void *a, *b;
+    int64_t a_stride, b_stride;
+    int64_t m, n, k;                 // out [m, n]
+    Epilogue e;
+    // A product may be cut along k: part s sums k from s * part_k on, and with
+    // more than one part each leaves its sums in parts[s] [m, round_up(n, 8)],
+    // for join_parts_kernel.
+    float* parts;
+    int64_t part_k;
+    int count;
+};
+
+// z -> out at row i, columns j .. j + 7, of which `left` exist; `z` is the
+// product, without the bias.
+template <typename T>
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t i, int64_t j, int left, float (&z)[8]) {
+    if (e.bias) {
+        const Eight<T> b = load_some(static_cast<const T*>(e.bias) + j, left);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z[c] += float(b[c]);
+    }
+    if (e.pre) store_some(static_cast<T*>(e.pre) + i * e.pre_stride + j, left, z);
+    if (e.act != FSDP_ACT_NONE)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z[c] = act_value(z[c], e.act);
+    if (e.times) {
+        const Eight<T> f = load_some(static_cast<const T*>(e.times) + i * e.times_stride + j, left);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z[c] *= float(f[c]);
+    }
+    if (e.residual) {
+        const Eight<T> r = load_some(static_cast<const T*>(e.residual) + i * e.residual_stride + j, left);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z[c] += float(r[c]);
+    }
+    store_some(static_cast<T*>(e.out) + i * e.out_stride + j, left, z);
+}
+
+// Eight finished or partial sums of row i, columns from j.  kPlain: the product
+// has no epilogue.
+template <typename T, bool kPlain>
+__device__ __forceinline__ void leave8(const Product& p, int part, int64_t i, int64_t j, float (&z)[8]) {
+    if (i >= p.m || j >= p.n) return;
+    const int left = int(min(p.n - j, int64_t(8)));
+    if (p.count > 1) {
+        const int64_t stride = (p.n + 7) / 8 * 8;
+        store_some(p.parts + (part * p.m + i) * stride + j, 8, z);
+    } else if constexpr (kPlain) {
+        store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
+    } else {
+        finish8<T>(p.e, i, j, left, z);
+    }
+}
+
+// The parts' sums, in order, and the epilogue: a thread takes eight columns.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(const Product p) {
+    const int64_t units = (p.n + 7) / 8, stride = units * 8;
+    for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < p.m * units; u += int64_t(gridDim.x) * 256) {
+        const int64_t i = u / units, j = u % units * 8;
+        float z[8] = {};
+        for (int s = 0; s < p.count; ++s) {
+            const Eight<float> v = load8(p.parts + (s * p.m + i) * stride + j);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[c] += v[c];
+        }
+        finish8<T>(p.e, i, j, int(min(p.n - j, int64_t(8))), z);
+    }
+}
+
+// ------------------------------------------------------------------ matrix cores
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 16 bytes of A rows and of B rows per lane -> a 32 x 32 tile.  Lane l holds
+// row l % 32 of both and the (l / 32)-th 16 bytes of a 32-byte run of k; element
+// r of lane l of the tile is at A row 8 (r / 4) + 4 (l / 32) + r % 4, B row l % 32.
+__device__ __forceinline__ f32x16 mma(Eight<bf16> a, Eight<bf16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(Eight<f16> a, Eight<f16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// 16 bytes of fp32 of A rows and of B rows per lane -> a 16 x 16 tile.  Lane l
+// holds row l % 16 of both and the (l / 16)-th 16 bytes of a 64-byte run of k;
+// element r of lane l of the tile is at A row 4 (l / 16) + r, B row l % 16.
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// Tile `id` of a launch: workgroups go to the 8 XCDs in turn, and each XCD has
+// an L2 of its own, so an XCD takes a run of tiles; in a run eight tiles of one
+// column of tiles follow each other, so that the 32 tiles in flight on an XCD
+// share eight strips of A and four of B.
+struct TilePlace {
+    int row, column, part;
+};
+__device__ __forceinline__ TilePlace tile_place(unsigned id, unsigned tiles_m, unsigned tiles_n, unsigned count) {
+    const unsigned all = tiles_m * tiles_n * count, xcd = id % 8, each = all / 8, more = all % 8;
+    id = xcd * each + min(xcd, more) + id / 8;
+    const unsigned part = id / (tiles_m * tiles_n);
+    id -= part * tiles_m * tiles_n;
+    constexpr unsigned kStrip = 8;
+    const unsigned strip = id / (kStrip * tiles_n), first = strip * kStrip, rows = min(kStrip, tiles_m - first);
+    id -= first * tiles_n;
+    return {int(first + id % rows), int(id / rows), int(part)};
+}
+
+// ------------------------------------------------------------------ the aligned product
+
+// A kTileM x kTileN tile of out in four waves, each a quarter of it.
+//
+// k goes by in steps of 64: 128 bytes of a row, a cache line (with steps of half
+// a line the L2 answers twice the requests: 1170 instead of 1300 TFLOP/s at
+// 8192 x 8192 x 8192).  kSteps steps of both operands lie in LDS.  A step is
+// worked on in two halves, two matrix instructions deep each, whose operands lie
+// in registers: while the matrix cores take one half the registers of the next
+// are read.  Once the second half of a step is in registers its place in LDS is
+// free for the step kSteps later, which then has the time of kSteps - 1 steps to
+// arrive.
+// Loads go from memory to LDS without passing registers; out of range they give
+// zeros, which is how odd sizes end.  A workgroup barrier a step.
+//
+// LDS layout, for conflict-free reads: "rows" 128 bytes per row, with the
+// 16-byte units of row r exchanged by r / 2; "columns" one run of columns per k,
+// its pairs of 32-byte blocks exchanged by k, read with the transposing load.
+template <int kRows, bool kColumns>
+struct Operand {
+    static constexpr int kBytes = kRows * 128;         // of a step
+    static constexpr int kLoads = kRows / 32;          // per thread and step, 16 bytes each
+    static constexpr int kUnits = kRows / 8;           // 16-byte units of one k of "columns"
+    __device__ static __forceinline__ int exchange(int k) { return kRows >= 128 ? (k & 3) * 2 : k & 2; }
+
+    const char* at;            // the step's first byte
+    int64_t step;              // bytes from a step to the next
+    int64_t left;              // bytes from `at` to the operand's end, in whole units
+    uint32_t offset[kLoads];
+    int k;                     // this lane's first k of a step ("rows")
+
+    __device__ __forceinline__ Operand(const void* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k1) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        if constexpr (kColumns) {
+            at = static_cast<const char*>(p) + (k0 * stride + first) * 2;
+            step = 64 * stride * 2;
+            left = (k1 - 1 - k0) * stride * 2 + (rows - first + 7) / 8 * 16;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int unit = (j * 4 + wave) * 64 + lane, kk = unit / kUnits, u = unit % kUnits;
+                offset[j] = uint32_t(kk * stride * 2 + ((u / 2 ^ exchange(kk)) * 2 + u % 2) * 16);
+            }
+            k = 0;
+        } else {
+            at = static_cast<const char*>(p) + (first * stride + k0) * 2;
+            step = 128;
+            left = (rows - 1 - first) * stride * 2 + (k1 - k0 + 7) / 8 * 16;
+            k = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int row = (j * 4 + wave) * 8 + lane / 8;
+                offset[j] = uint32_t(row * stride * 2 + k * 2);
+            }
+        }
+    }
+
+    // Asks for the next step, with `rest` k left, into `lds`.
+    __device__ __forceinline__ void load(char* lds, int64_t rest) {
+        typedef __attribute__((address_space(3))) void lds_void;
+        constexpr uint32_t kMost = 0x7ffffff0u, kNowhere = 0xfffffff0u;
+        const uint32_t bytes = rest <= 0 ? 0u : uint32_t(min(left, int64_t(kMost)));
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, int(bytes), 0x00020000);
+        const bool mine = kColumns || k < rest;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + (j * 4 + (threadIdx.x >> 6)) * 1024), 16,
+                                                     int(mine ? offset[j] : kNowhere), 0, 0, 0);
+        at += step;
+        left -= step;
+    }
+};
+
+// A wave's registers of half a step: kTiles times 32 rows of an operand, for
+// two matrix instructions each.
+template <typename T, int kRows, bool kColumns, int kTiles>
+struct Fragments {
+    static constexpr int kPlaces = kColumns ? kTiles : 4;
+    Eight<T> v[2][kTiles];
+    // This lane's places in a step's LDS, of the wave whose first row is `first`.
+    __device__ static __forceinline__ void lane_places(int first, int (&place)[kPlaces]) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int x = 0; x < kPlaces; ++x) {
+            if constexpr (kColumns) {
+                const int k = lane / 32 * 8 + lane % 16 / 4, block = first / 16 + 2 * x + lane / 16 % 2;
+                place[x] = k * kRows * 2 + (block ^ Operand<kRows, true>::exchange(k)) * 32 + lane % 4 * 8;
+            } else {
+                place[x] = (first + lane % 32) * 128 + ((2 * x + lane / 32) ^ lane / 2 % 8) * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void read(const char* lds, const int (&place)[kPlaces], int half) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < kTiles; ++x) {
+                if constexpr (kColumns) {
+                    // The transposing load gives lane i of 16 the i-th column of the 4 x 16 block that the 16 lanes point to.
+                    const char* const at = lds + place[x] + (2 * half + h) * 16 * kRows * 2;
+                    v[h][x] = __builtin_bit_cast(Eight<T>, __builtin_shufflevector(
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at),
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRows * 2)), 0, 1, 2, 3, 4, 5, 6, 7));
+                } else {
+                    v[h][x] = *reinterpret_cast<const Eight<T>*>(lds + place[2 * half + h] + x * 32 * 128);
+                }
+            }
+    }
+};
+
+template <typename T, bool kColumnsA, bool kColumnsB, int kTileM, int kTileN, int kSteps>
+__global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void product_kernel(const Product p) {
+    using A = Operand<kTileM, kColumnsA>;
+    using B = Operand<kTileN, kColumnsB>;
+    constexpr int kA = kTileM / 64, kB = kTileN / 64;            // 32-row tiles of a wave
+    // One array per step: their reads and loads are known not to touch each other.
+    __shared__ __attribute__((aligned(1024))) char a0[A::kBytes], a1[A::kBytes], a2[kSteps > 2 ? A::kBytes : 16],
+        a3[kSteps > 2 ? A::kBytes : 16], b0[B::kBytes], b1[B::kBytes], b2[kSteps > 2 ? B::kBytes : 16], b3[kSteps > 2 ? B::kBytes : 16];
+    static_assert(kSteps == 2 || kSteps == 4);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wi = wave / 2 * (kTileM / 2), wj = wave % 2 * (kTileN / 2);
+    const TilePlace t = tile_place(blockIdx.x, unsigned((p.m + kTileM - 1) / kTileM), unsigned((p.n + kTileN - 1) / kTileN),
+                                   unsigned(p.count));
+    const int64_t i0 = int64_t(t.row) * kTileM, j0 = int64_t(t.column) * kTileN;
+    const int64_t k0 = t.part * p.part_k, k1 = min(k0 + p.part_k, p.k);
+    A a(p.a, p.a_stride, i0, p.m, k0, k1);
+    B b(p.b, p.b_stride, j0, p.n, k0, k1);
+    using FA = Fragments<T, kTileM, kColumnsA, kA>;
+    using FB = Fragments<T, kTileN, kColumnsB, kB>;
+    FA fa[2];
+    FB fb[2];
+    int pa[FA::kPlaces], pb[FB::kPlaces];
+    FA::lane_places(wi, pa);
+    FB::lane_places(wj, pb);
+    f32x16 acc[kA][kB] = {};
+
+    // Waits for this wave's loads, but for those of the last kLater steps, and
+    // its LDS reads; then for the other waves.
+    const auto sync = [](auto later) {
+        constexpr int n = decltype(later)::value * (A::kLoads + B::kLoads);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 7 << 4);        // vmcnt(n) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int64_t rest = k1 - k0;                                       // k not yet asked for
+    const auto ask = [&](char* la, char* lb) {
+        a.load(la, rest);
+        b.load(lb, rest);
+        rest -= 64;
+    };
+    constexpr int kMma = 2 * kA * kB, kReads = 2 * kA * (kColumnsA ? 2 : 1) + 2 * kB * (kColumnsB ? 2 : 1),
+                  kLoads = A::kLoads + B::kLoads;
+    // Half a step: the order of issue is LDS reads first, under the matrix
+    // instructions, which then have the rest of the half to arrive; the memory
+    // loads after them.
+    const auto half = [&](const FA& xa, const FB& xb, auto loads) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < kA; ++x)
+#pragma unroll
+                for (int y = 0; y < kB; ++y) acc[x][y] = mma(xa.v[h][x], xb.v[h][y], acc[x][y]);
+        if constexpr (decltype(loads)::value) {
+            constexpr int kTurns = kLoads, kEach = kMma / kTurns > 0 ? kMma / kTurns : 1;
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kTurns - 1) / kTurns, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+            }
+        } else {
+            constexpr int kFew = (kReads + kMma / 2 - 1) / (kMma / 2);
+#pragma unroll
+            for (int i = 0; i < kReads; i += kFew) {
+                __builtin_amdgcn_sched_group_barrier(0x100, kFew, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+        }
+    };
+    // A step that lies in (la, lb), the next one in (ma, mb).
+    const auto step = [&](char* la, char* lb, char* ma, char* mb) {
+        fa[1].read(la, pa, 1);
+        fb[1].read(lb, pb, 1);
+        half(fa[0], fb[0], std::false_type());
+        sync(std::integral_constant<int, kSteps - 2>());
+        ask(la, lb);
+        fa[0].read(ma, pa, 0);
+        fb[0].read(mb, pb, 0);
+        half(fa[1], fb[1], std::true_type());
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    ask(a0, b0);
+    ask(a1, b1);
+    if constexpr (kSteps > 2) {
+        ask(a2, b2);
+        ask(a3, b3);
+    }
+    sync(std::integral_constant<int, kSteps - 1>());
+    fa[0].read(a0, pa, 0);
+    fb[0].read(b0, pb, 0);
+    // Steps past the end add zeros: the loop takes kSteps at a time.
+    for (int64_t left = k1 - k0; left > 0; left -= 64 * kSteps) {
+        step(a0, b0, a1, b1);
+        if constexpr (kSteps == 2) {
+            step(a1, b1, a0, b0);
+        } else {
+            step(a1, b1, a2, b2);
+            step(a2, b2, a3, b3);
+            step(a3, b3, a0, b0);
+        }
+    }
+    sync(std::integral_constant<int, 0>());                       // nothing more is written to LDS
+
+    // A wave passes its sums through its own piece of LDS, 32 rows at a time, so
+    // that a lane gets eight neighbouring columns; every other four rows have
+    // their halves of 32 columns exchanged, against conflicts.
+    constexpr int kWide = kTileN / 2, kLanes = kWide / 8;
+    static_assert(B::kBytes == 2 * 32 * kWide * 4 && kWide >= 64, "two waves' pieces");
+    float* const turn = reinterpret_cast<float*>(wave < 2 ? b0 : b1) + wave % 2 * 32 * kWide;
+    const auto place = [](int row, int column) { return row * kWide + (column ^ (row / 4 % 2) * 32); };
+#pragma unroll
+    for (int x = 0; x < kA; ++x) {
+#pragma unroll
+        for (int y = 0; y < kB; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                turn[place(8 * (r / 4) + 4 * (lane / 32) + r % 4, 32 * y + lane % 32)] = acc[x][y][r];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
+            const int column = lane % kLanes * 8;
+            float z[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[c] = turn[place(r, column) + c];
+            leave8<T, kColumnsB>(p, t.part, i0 + wi + 32 * x + r, j0 + wj + column, z);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+}  // namespace
+}  // namespace fsdp_block
