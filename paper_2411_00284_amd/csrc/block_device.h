@@ -56,16 +56,35 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&in)[8]) {
         if (i < n) p[i] = v[i];
 }
 
-// The same order of additions in every call: results do not depend on timing.
+// Reductions over a wave in six steps through the lanes' own data paths (DPP):
+// four within rows of 16 lanes, two that pass a row's last lane on.  The result
+// is that of lane 63, for all lanes.  The order of additions is fixed: results do
+// not depend on timing.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float lanes_moved(float v, float none) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), kCtrl,
+                                                                 kRows, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    v += lanes_moved<0x111, 0xf>(v, 0.f);        // from 1, 2, 4, 8 lanes below
+    v += lanes_moved<0x112, 0xf>(v, 0.f);
+    v += lanes_moved<0x114, 0xf>(v, 0.f);
+    v += lanes_moved<0x118, 0xf>(v, 0.f);
+    v += lanes_moved<0x142, 0xa>(v, 0.f);        // rows 0 and 2 into 1 and 3
+    v += lanes_moved<0x143, 0xc>(v, 0.f);        // row 1 into 2 and 3
+    return last_lane(v);
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    v = fmaxf(v, lanes_moved<0x111, 0xf>(v, v));
+    v = fmaxf(v, lanes_moved<0x112, 0xf>(v, v));
+    v = fmaxf(v, lanes_moved<0x114, 0xf>(v, v));
+    v = fmaxf(v, lanes_moved<0x118, 0xf>(v, v));
+    v = fmaxf(v, lanes_moved<0x142, 0xa>(v, v));
+    v = fmaxf(v, lanes_moved<0x143, 0xc>(v, v));
+    return last_lane(v);
 }
 
 // Sums of kN values over a workgroup of kThreads, for all threads.  `part`

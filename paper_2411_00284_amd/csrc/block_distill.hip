@@ -2,9 +2,9 @@
 // (include/fsdp_block.h).
 //
 // Bound by HBM: a row of logits is read for its maximum and sum (kept running
-// together, in one pass) and again for its gradient; the second read comes
-// from cache.  A workgroup takes a row; the teacher's entries, at most 1024,
-// lie in LDS.
+// together, in one pass), and again for its gradient; a workgroup takes a row
+// and holds what it can of it in registers, so that the second read is of the
+// rest only, from cache.  The teacher's entries, at most 1024, lie in LDS.
 
 #include "block_device.h"
 #include "block_host.h"
@@ -40,29 +40,146 @@ __device__ __forceinline__ int id_at(const DistillArgs& a, int64_t i) {
     return id < 0 ? -1 : id > INT32_MAX ? INT32_MAX : int(id);
 }
 
-// The running maximum m and sum of 2^((s - m) c) of a softmax.  A maximum of
-// -inf counts as 0 in the exponents, so that rows and threads that hold nothing
-// but -inf (or nothing) keep a sum of 0.
-__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ void join_softmax(float& m, float& s, float m2, float s2, float c) {
-    const float top = fmaxf(m, m2), z = shift_of(top);
-    s = s * exp2f((m - z) * c) + s2 * exp2f((m2 - z) * c);
-    m = top;
+// 2^x by the hardware's instruction, to one unit of the last place; results
+// below the smallest normal number are 0.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The running maximum m and sum s of a softmax, over terms 2^(v c - m c) with
+// m c rounded: one multiply-add and one exponential a term.  A maximum of -inf
+// counts as 0 in the exponents, so that threads that hold nothing but -inf (or
+// nothing) keep a sum of 0.
+struct Softmax {
+    float m = -INFINITY, s = 0.f;
+    __device__ static __forceinline__ float shift(float m, float c) { return m == -INFINITY ? 0.f : m * c; }
+    __device__ __forceinline__ void join(float m2, float s2, float c) {
+        const float top = fmaxf(m, m2), z = shift(top, c);
+        // A sum of 0 stays one, whatever its maximum.
+        s = (s == 0.f ? 0.f : s * exp2_fast(shift(m, c) - z)) + (s2 == 0.f ? 0.f : s2 * exp2_fast(shift(m2, c) - z));
+        m = top;
+    }
+};
+
+// log2(v) in 64 bits to about 2^-24: the exponent is exact, the mantissa's
+// logarithm is below one half.
+__device__ __forceinline__ double log2_of(float v) {
+    int e;
+    const float f = frexpf(v, &e);                              // v = f 2^e, f in [1/2, 1)
+    const bool low = f < 0.70710678f;
+    return v == 0.f || !isfinite(v) ? double(__builtin_amdgcn_logf(v))
+                                    : double(low ? e - 1 : e) + double(__builtin_amdgcn_logf(low ? f + f : f));
 }
 
-template <typename T, int kThreads>
-__global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a) {
-    constexpr int kWaves = kThreads / 64;
+// A thread's share of a row: whole 16-byte units, a unit of a thread kThreads
+// units from its next, and one of the elements after them.  Units past the row's
+// hold -inf, which no maximum and no sum notices.
+template <typename T>
+struct Unit {
+    static constexpr int n = 16 / int(sizeof(T));
+    typedef T vec __attribute__((ext_vector_type(n)));
+    typedef vec any __attribute__((aligned(sizeof(T))));
+    vec v;
+    // kLast: the bytes are not needed again.
+    template <bool kLast = false>
+    __device__ __forceinline__ void load(const T* s, int unit, int units) {
+        if (unit < units) {
+            const any* const at = reinterpret_cast<const any*>(s + unit * n);
+            v = kLast ? __builtin_nontemporal_load(at) : *at;
+        } else {
+            v = vec(T(-INFINITY));
+        }
+    }
+    // Past the caches: the gradient's next reader comes after the whole of it.
+    // (The units that an entry is written into again, through the caches: 528
+    // instead of 445 us at 4096 x 128256; all units so: 530.)
+    __device__ __forceinline__ static void store(T* s, int unit, vec out) {
+        __builtin_nontemporal_store(out, reinterpret_cast<any*>(s + unit * n));
+    }
+};
+
+constexpr int kTogether = 2;                     // units streamed at a time
+
+template <typename T, int kUnits>
+__device__ __forceinline__ void add_units(Softmax& x, const Unit<T> (&u)[kUnits], float c) {
+    float most = x.m;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k)
+#pragma unroll
+        for (int i = 0; i < Unit<T>::n; ++i) most = fmaxf(most, float(u[k].v[i]));
+    const float z = Softmax::shift(most, c);
+    if (most > x.m && x.s != 0.f) x.s *= exp2_fast(Softmax::shift(x.m, c) - z);
+    x.m = most;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k)
+#pragma unroll
+        for (int i = 0; i < Unit<T>::n; ++i) x.s += exp2_fast(float(u[k].v[i]) * c - z);
+}
+
+// f(entry, sum of p over the entries with its id).  Repeated ids are found
+// in LDS: an entry that is alone in its slot of a table is no repeat, others are
+// put into another table, and what still shares a slot after kRounds looks at
+// all entries.  (All pairs at once: 160 us of 660 at 4096 rows of 512 entries.)
+constexpr int kSlots = 2048, kRounds = 3, kFewEntries = 96;
+template <int kThreads, typename F>
+__device__ __forceinline__ void for_same_ids(int top, const int* ids, const float* p, int* slots, F f) {
+    constexpr int kEntries = FSDP_DISTILL_MAX_TOP / kThreads;
+    uint32_t open = ~0u;                         // a bit per entry of this thread
+    if (top > kFewEntries) {
+        for (int round = 0; round < kRounds; ++round) {
+            for (int i = threadIdx.x; i < kSlots; i += kThreads) slots[i] = 0;
+            __syncthreads();
+            const unsigned mix = round == 0 ? 2654435761u : round == 1 ? 2246822519u : 3266489917u;
+            const auto slot = [&](int k) { return &slots[unsigned(ids[k]) * mix >> 21]; };
+            const auto is_open = [&](int e, int k) { return k < top && ids[k] >= 0 && (open >> e & 1); };
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (const int k = int(threadIdx.x) + e * kThreads; is_open(e, k)) atomicAdd(slot(k), 1);
+            __syncthreads();
+            uint32_t still = 0;
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (const int k = int(threadIdx.x) + e * kThreads; is_open(e, k) && *slot(k) > 1) still |= 1u << e;
+            open = still;
+            if (!__syncthreads_or(int(open))) break;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        const int k = int(threadIdx.x) + e * kThreads;
+        if (k >= top || ids[k] < 0) continue;
+        float same = p[k];
+        if (open >> e & 1) {
+            const int id = ids[k];
+            same = 0.f;
+            for (int i = 0; i < top; ++i) same += ids[i] == id ? p[i] : 0.f;
+        }
+        f(k, same);
+    }
+}
+
+// kHeld units per thread stay in registers; those of the first group are asked
+// for before the teacher's entries are looked at.
+template <typename T, int kThreads, int kHeld>
+__global__ __launch_bounds__(kThreads, 4) void distill_kernel(const DistillArgs a) {
+    constexpr int kWaves = kThreads / 64, n = Unit<T>::n;
+    static_assert(kHeld >= 4 && kHeld % 2 == 0);
     __shared__ float p[FSDP_DISTILL_MAX_TOP], picked[FSDP_DISTILL_MAX_TOP];
-    __shared__ int ids[FSDP_DISTILL_MAX_TOP];
-    __shared__ float wm[kWaves], ws[kWaves];
+    __shared__ int ids[FSDP_DISTILL_MAX_TOP], slots[kSlots];
+    __shared__ float wm[kWaves], ws[kWaves], wt[kWaves], wp[kWaves];
     __shared__ double wd[kWaves];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, vocab = a.vocab, units = vocab / n;
+    const int single = units * n + t;                           // this thread's element after the units
     const float c = kLog2e / a.tau;
+    const double tau = double(a.tau), per_tau = 1.0 / tau, ln2 = 0.6931471805599453;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
-        const T* s = static_cast<const T*>(a.logits) + row * a.logits_stride;
-        T* ds = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-        // The teacher's softmax.
+        const T* const s = static_cast<const T*>(a.logits) + row * a.logits_stride;
+        T* const ds = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+        const float weight = a.dlogits ? a.dloss[row] : 0.f;
+        Unit<T> held[kHeld / 2][2];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) held[u / 2][u % 2].load(s, t + u * kThreads, units);
+        const float lone = single < vocab ? float(s[single]) : -INFINITY;
+        // The teacher's entries: id, logit, the student's logit there (which an in-place gradient overwrites).
+        // Each is its thread's own, from here to the end.
         float top = -INFINITY;
         int bad = 0;
         for (int k = t; k < a.top; k += kThreads) {
@@ -70,111 +187,125 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(const DistillArgs a) 
             const float v = id < 0 ? -INFINITY : teacher_at(a, row * a.top + k);
             ids[k] = id;
             p[k] = v;
-            picked[k] = id >= 0 && id < a.vocab ? float(s[id]) : 0.f;
-            bad |= id >= a.vocab;
+            picked[k] = id >= 0 && id < vocab ? float(s[id]) : 0.f;
+            bad |= id >= vocab;
             top = v != v || top != top ? NAN : fmaxf(top, v);
         }
         top = __any(top != top) ? NAN : wave_max(top);
         if (lane == 0) wm[wave] = top;
         bad = __syncthreads_or(bad);
         for (int w = 0; w < kWaves; ++w) top = wm[w] != wm[w] || top != top ? NAN : fmaxf(top, wm[w]);
-        const bool none = top == -INFINITY;                     // no entry, or none with any mass
-        const float scale = a.dlogits ? a.dloss[row] * a.tau : 0.f;
-        if (none || bad) {
+        if (top == -INFINITY || bad) {                          // no entry with any mass, or one out of range
             const float fill = bad ? NAN : 0.f;
             if (t == 0 && a.loss) a.loss[row] = fill;
             if (t == 0 && a.lse) a.lse[row] = 0.f;
-            if (a.dlogits)
-                for (int j = t; j < a.vocab; j += kThreads) ds[j] = T(fill);
+            if (a.dlogits) {
+                for (int u = t; u < units; u += kThreads) Unit<T>::store(ds, u, typename Unit<T>::vec(T(fill)));
+                if (single < vocab) ds[single] = T(fill);
+            }
             __syncthreads();                                    // LDS is the next row's
             continue;
         }
-        float one[1] = {0.f};
-        for (int k = t; k < a.top; k += kThreads) one[0] += exp2f((p[k] - top) * c);
-        group_sum<kThreads, 1>(one, ws);
-        const double teacher_lse = a.teacher_lse ? double(a.teacher_lse[row]) : double(top) / double(a.tau) + log(double(one[0]));
-        // The student's softmax.
-        double lse;
-        if (a.lse_in) {
-            lse = double(a.lse_in[row]);
-        } else {
-            float m = -INFINITY, sum = 0.f;
-            for (int j = t * 8; j < a.vocab; j += kThreads * 8) {
-                const int left = a.vocab - j;
-                const Eight<T> v = load_some(s + j, left);
-                float most = float(v[0]);
-#pragma unroll
-                for (int i = 1; i < 8; ++i)
-                    if (i < left) most = fmaxf(most, float(v[i]));
-                const float next = fmaxf(m, most), z = shift_of(next);
-                sum *= exp2f((m - z) * c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < left) sum += exp2f((float(v[i]) - z) * c);
-                m = next;
-            }
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) join_softmax(m, sum, __shfl_xor(m, d), __shfl_xor(sum, d), c);
-            __syncthreads();                                    // ws has been read
-            if (lane == 0) {
-                wm[wave] = m;
-                ws[wave] = sum;
-            }
-            __syncthreads();
-            m = -INFINITY;
-            sum = 0.f;
-            for (int w = 0; w < kWaves; ++w) join_softmax(m, sum, wm[w], ws[w], c);
-            lse = double(m) / double(a.tau) + log(double(sum));
-        }
-        if (t == 0 && a.lse) a.lse[row] = float(lse);
-        // p_k, their sum and the loss.
-        const float shift = float(teacher_lse * double(a.tau) - double(top));      // p_k = exp((v_k - top - shift) / tau)
-        float mass = 0.f;
-        double loss = 0.0;
-        for (int k = t; k < a.top; k += kThreads) {
-            const float v = p[k], pk = exp2f(((v - top) - shift) * c);
-            mass += pk;
-            p[k] = pk;
-            if (pk != 0.f) loss += double(pk) * ((double(v) - double(picked[k])) / double(a.tau) - (teacher_lse - lse));
+        // What depends on the entries alone is left to the waves that hold some.
+        const bool some = wave * 64 < a.top;
+        float sum = 0.f;
+        if (some) {
+            for (int k = t; k < a.top; k += kThreads) sum += exp2_fast((p[k] - top) * c);
+            sum = wave_sum(sum);
         }
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            mass += __shfl_xor(mass, d);
-            loss += __shfl_xor(loss, d);
+        for (int u = 4; u < kHeld; ++u) held[u / 2][u % 2].load(s, t + u * kThreads, units);
+        Softmax x;
+        if (!a.lse_in) {
+#pragma unroll
+            for (int u = 0; u < kHeld / 2; ++u) add_units(x, held[u], c);
+            for (int j = t + kHeld * kThreads; j < units; j += kTogether * kThreads) {
+                Unit<T> u[kTogether];
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) u[k].load(s, j + k * kThreads, units);
+                add_units(x, u, c);
+            }
+            x.join(lone, lone == -INFINITY ? 0.f : 1.f, c);
+            // Over the wave: the maximum first, then sums of one shift.
+            const float m = wave_max(x.m), z = Softmax::shift(m, c);
+            x.s = wave_sum(x.s == 0.f ? 0.f : x.s * exp2_fast(Softmax::shift(x.m, c) - z));
+            x.m = m;
+        }
+        __syncthreads();                                        // wm has been read
+        if (lane == 0) {
+            wt[wave] = sum;
+            wm[wave] = x.m;
+            ws[wave] = x.s;
         }
         __syncthreads();
+        x = Softmax();
+        sum = 0.f;
+        for (int w = 0; w < kWaves; ++w) {
+            sum += wt[w];
+            if (!a.lse_in) x.join(wm[w], ws[w], c);
+        }
+        const double teacher = a.teacher_lse ? double(a.teacher_lse[row]) : double(top) * per_tau + log2_of(sum) * ln2;
+        // The rounding of m c, which the sum's terms had, is taken out of its logarithm.
+        const float lost = x.m == -INFINITY ? 0.f : fmaf(x.m, c, -Softmax::shift(x.m, c));
+        const double lse = a.lse_in ? double(a.lse_in[row]) : double(x.m) * per_tau + (log2_of(x.s) - double(lost)) * ln2;
+        if (t == 0 && a.lse) a.lse[row] = float(lse);
+        // p_k, their sum and the loss.
+        const float rest = float(teacher * tau - double(top));  // p_k = exp((v_k - top - rest) / tau)
+        float mass = 0.f;
+        double loss = 0.0;
+        if (some) {
+            for (int k = t; k < a.top; k += kThreads) {
+                const float v = p[k], pk = exp2_fast(((v - top) - rest) * c);
+                mass += pk;
+                if (pk != 0.f) loss += double(pk) * ((double(v) - double(picked[k])) * per_tau - (teacher - lse));
+                p[k] = pk;
+            }
+            mass = wave_sum(mass);
+            if (a.loss)
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+        }
         if (lane == 0) {
-            ws[wave] = mass;
+            wp[wave] = mass;
             wd[wave] = loss;
         }
         __syncthreads();
-        mass = 0.f;
-        loss = 0.0;
-        for (int w = 0; w < kWaves; ++w) {
-            mass += ws[w];
-            loss += wd[w];
+        if (t == 0 && a.loss) {
+            loss = 0.0;
+            for (int w = 0; w < kWaves; ++w) loss += wd[w];
+            a.loss[row] = float(tau * tau * loss);
         }
-        if (t == 0 && a.loss) a.loss[row] = float(double(a.tau) * double(a.tau) * loss);
         if (a.dlogits) {
-            // q = exp((s - base - rest) / tau): the logsumexp in two parts, so that
-            // logits far from 0 lose nothing.
-            const float base = float(lse * double(a.tau)), rest = float(lse * double(a.tau) - double(base));
-            const bool zero = a.dloss[row] == 0.f;
-            for (int j = t * 8; j < a.vocab; j += kThreads * 8) {
-                const Eight<T> v = load_some(s + j, a.vocab - j);
-                float out[8];
+            mass = 0.f;
+            for (int w = 0; w < kWaves; ++w) mass += wp[w];
+            // q = 2^(s c - b): b in two parts, the second as a factor
+            const double b = lse * tau * double(c);
+            const float base = float(b), scale = weight * a.tau;
+            const bool zero = weight == 0.f;
+            const float factor = scale * mass * exp2_fast(float(double(base) - b));
+            const auto slope = [&](float v) { return T(zero ? 0.f : factor * exp2_fast(v * c - base)); };
+            const auto put = [&](const Unit<T>& u, int unit) {
+                if (unit >= units) return;
+                typename Unit<T>::vec out;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) out[i] = zero ? 0.f : scale * mass * exp2f(((float(v[i]) - base) - rest) * c);
-                store_some(ds + j, a.vocab - j, out);
+                for (int i = 0; i < n; ++i) out[i] = slope(float(u.v[i]));
+                Unit<T>::store(ds, unit, out);
+            };
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u) put(held[u / 2][u % 2], t + u * kThreads);
+            for (int j = t + kHeld * kThreads; j < units; j += kTogether * kThreads) {
+                Unit<T> u[kTogether];
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) u[k].template load<true>(s, j + k * kThreads, units);
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) put(u[k], j + k * kThreads);
             }
+            if (single < vocab) ds[single] = slope(lone);
             __syncthreads();                                    // the entries' places are written again
-            if (!zero)
-                for (int k = t; k < a.top; k += kThreads) {
-                    if (ids[k] < 0) continue;
-                    float same = 0.f;
-                    for (int i = 0; i < a.top; ++i) same += ids[i] == ids[k] ? p[i] : 0.f;
-                    ds[ids[k]] = T(scale * (mass * exp2f(((picked[k] - base) - rest) * c) - same));
-                }
+            if (!zero)                                          // the same for the whole workgroup
+                for_same_ids<kThreads>(a.top, ids, p, slots, [&](int k, float same) {
+                    ds[ids[k]] = T(factor * exp2_fast(picked[k] * c - base) - scale * same);
+                });
         }
         __syncthreads();                                        // LDS is the next row's
     }
@@ -212,10 +343,23 @@ fsdp_status run(const fsdp_distill_args* args, bool backward, hipStream_t stream
                         backward ? nullptr : a.loss, backward ? nullptr : a.lse, a.dlogits, a.logits_stride,
                         a.dlogits_stride, t, int(a.vocab), int(a.top), a.teacher_dtype, a.ids_64, a.temperature};
     const dim3 grid(unsigned(std::min<int64_t>(t, int64_t(1) << 21)));
+    fsdp_status found = FSDP_OK;
+    const int cus = cu_count(&found);
+    if (cus == 0) return found;
+    // Few rows: as many threads as a workgroup has, each with more of the row on
+    // its way at once.  Else 256 threads, the most workgroups that a row's chain of
+    // loads and sums can hide behind; for a row that is read twice and long, 512,
+    // which hold twice of it (at 4096 x 128256 in bf16, loss and gradient: 445
+    // instead of 488 us; the loss alone 210 instead of 191, and at 8192 x 32000 both
+    // 247 instead of 224).
+    const int64_t units = ceil_div(a.vocab, 16 / elem_bytes(a.dtype));
+    const bool twice = !backward && a.dlogits;
     const auto of = [&](auto type) {
         using T = decltype(type);
-        return a.vocab <= 8192 ? launch(distill_kernel<T, 256>, k, grid, 256, stream)
-                               : launch(distill_kernel<T, 1024>, k, grid, 1024, stream);
+        if (t <= cus) return launch(distill_kernel<T, 1024, 8>, k, grid, 1024, stream);
+        if (units <= 4 * 256) return launch(distill_kernel<T, 256, 4>, k, grid, 256, stream);
+        if (!twice || units <= 4096) return launch(distill_kernel<T, 256, 8>, k, grid, 256, stream);
+        return launch(distill_kernel<T, 512, 8>, k, grid, 512, stream);
     };
     return a.dtype == FSDP_DTYPE_BF16 ? of(bf16(0.f)) : a.dtype == FSDP_DTYPE_F16 ? of(f16(0.f)) : of(0.f);
 }
