@@ -117,8 +117,9 @@ __device__ __forceinline__ void add_units(Softmax& x, const Unit<T> (&u)[kUnits]
 // f(entry, sum of p over the entries with its id).  Repeated ids are found
 // in LDS: an entry that is alone in its slot of a table is no repeat, others are
 // put into another table, and what still shares a slot after kRounds looks at
-// all entries.  (All pairs at once: 160 us of 660 at 4096 rows of 512 entries.)
-constexpr int kSlots = 2048, kRounds = 3, kFewEntries = 96;
+// all entries.  (All pairs at once: 160 us of 660 at 4096 rows of 512 entries; six tables leave
+// hardly one of 1024 different ids to the last step.)
+constexpr int kSlots = 2048, kRounds = 6, kFewEntries = 16;
 template <int kThreads, typename F>
 __device__ __forceinline__ void for_same_ids(int top, const int* ids, const float* p, int* slots, F f) {
     constexpr int kEntries = FSDP_DISTILL_MAX_TOP / kThreads;
@@ -127,7 +128,7 @@ __device__ __forceinline__ void for_same_ids(int top, const int* ids, const floa
         for (int round = 0; round < kRounds; ++round) {
             for (int i = threadIdx.x; i < kSlots; i += kThreads) slots[i] = 0;
             __syncthreads();
-            const unsigned mix = round == 0 ? 2654435761u : round == 1 ? 2246822519u : 3266489917u;
+            const unsigned mix = 2654435761u + 2246822518u * unsigned(round);       // odd: a table of its own
             const auto slot = [&](int k) { return &slots[unsigned(ids[k]) * mix >> 21]; };
             const auto is_open = [&](int e, int k) { return k < top && ids[k] >= 0 && (open >> e & 1); };
 #pragma unroll
