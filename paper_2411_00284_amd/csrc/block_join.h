@@ -17,7 +17,9 @@ struct JoinArgs {
     int hidden;
 };
 
-constexpr int kJoinColumns = 64, kJoinThreads = 1024;
+// A line of 32 columns per workgroup and 32 rows of parts at a time: many
+// workgroups, each with few loads to wait for one after the other.
+constexpr int kJoinColumns = 32, kJoinThreads = 1024;
 
 template <typename TB>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const JoinArgs a) {

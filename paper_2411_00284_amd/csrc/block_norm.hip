@@ -122,137 +122,223 @@ struct NormGradArgs {
     void *dx, *dbranch, *dgate;
     float *part_pre, *part_post, *part_gate;     // [units, hidden], or NULL
     int64_t y_stride, dy_stride, dh_stride, branch_stride, dx_stride, dbranch_stride;
-    int64_t tokens, group_rows, units, unit_rows;
+    int64_t tokens, group_rows, unit_rows;
     int64_t units_per_group;                     // > 0: a unit's rows share one row of the gate
     int hidden;
     float eps, residual_scale, branch_scale;
 };
 
-// A team takes a unit of consecutive rows and sums the weights' gradients over
-// them in registers; the units' sums are joined by join_kernel, in order.
+// A workgroup takes a unit of consecutive rows and sums the weights' gradients
+// over them in registers; the units' sums are joined by join_kernel, in order.
+// While a row is worked on the next one is on its way.  A row needs one round of
+// sums over the team: with c = branch_scale * gate * post_weight * branch, the
+// inner product of c with the gradient of y is that of c with dy, dh * pre_weight
+// and y, weighted by row statistics that the same round gives.
 template <typename TX, typename TB, typename TW, int kTeam, int kChunks>
 __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const NormGradArgs a) {
-    __shared__ float part[2][3 * (kTeam / 64)];
-    const int t = threadIdx.x % kTeam;
+    // 1024 threads have 128 registers each: two chunks leave no room for the next
+    // row, the weights and the weights' sums, which then lie in LDS (in registers
+    // they spilled: 855 instead of %s us at 4096 x 16384).
+    constexpr bool kRoomy = kTeam < 1024 || kChunks == 1;
+    constexpr int kGroup = kTeams<kTeam>;
+    __shared__ float part[2][6 * (kTeam / 64)];
+    __shared__ float joined[kGroup > 1 ? kGroup : 1][kGroup > 1 ? kTeam * kChunks * 8 : 1];
+    const int t = threadIdx.x % kTeam, team = threadIdx.x / kTeam;
     const int hidden = a.hidden;
-    const int64_t unit = int64_t(blockIdx.x) * kTeams<kTeam> + threadIdx.x / kTeam;
-    if (unit >= a.units) return;                 // a whole team; teams share a barrier only where they are workgroups
-    int64_t lo, hi, group = 0;
-    if (a.units_per_group > 0) {
+    const int64_t unit = blockIdx.x;
+    // Rows by `run`s, one to a team in turn: a row of the gate's tokens where the unit holds whole ones, else one.
+    int64_t lo, hi, group = 0, run = 1;
+    const bool whole = a.units_per_group == 0;
+    if (!whole) {
         group = unit / a.units_per_group;
         lo = group * a.group_rows + unit % a.units_per_group * a.unit_rows;
         hi = min(lo + a.unit_rows, (group + 1) * a.group_rows);
     } else {
         lo = unit * a.unit_rows;
         hi = min(lo + a.unit_rows, a.tokens);
-        if (a.gate) group = lo / a.group_rows;
+        if (a.gate) {
+            run = a.group_rows;
+            group = lo / run + team;
+        }
     }
-    int64_t in_group = 0;                        // rows of the group so far
-    float dpre[kChunks][8] = {}, dpost[kChunks][8] = {}, dgate[kChunks][8] = {};
-    int flip = 0;
-    for (int64_t row = lo; row < hi; ++row) {
+    struct Row {
         Eight<TX> y[kChunks], dy[kChunks];
         Eight<TB> dh[kChunks], b[kChunks];
-        float s[3] = {0.f, 0.f, 0.f};            // sums of y^2, dh * w * y, branch^2
+    };
+    const auto load = [&](Row& r, int64_t row) {
         FSDP_CHUNKS(c, at, left) {
-            if (a.dy) dy[c] = load_some(row_of<TX>(a.dy, row, a.dy_stride) + at, left);
+            if (a.dy) r.dy[c] = load_some(row_of<TX>(a.dy, row, a.dy_stride) + at, left);
             if (a.dh) {
-                y[c] = load_some(row_of<TX>(a.y, row, a.y_stride) + at, left);
-                dh[c] = load_some(row_of<TB>(a.dh, row, a.dh_stride) + at, left);
+                r.y[c] = load_some(row_of<TX>(a.y, row, a.y_stride) + at, left);
+                r.dh[c] = load_some(row_of<TB>(a.dh, row, a.dh_stride) + at, left);
             }
-            if (a.branch) b[c] = load_some(row_of<TB>(a.branch, row, a.branch_stride) + at, left);
+            if (a.branch) r.b[c] = load_some(row_of<TB>(a.branch, row, a.branch_stride) + at, left);
         }
-        FSDP_CHUNKS(c, at, left) {
-            if (a.dh) {
-                const Eight<TW> w = load_some(static_cast<const TW*>(a.pre) + at, left);
+    };
+    Eight<TW> wy[kChunks], wb[kChunks];
+    Eight<TB> gate[kChunks];
+    const auto load_weights = [&](int c, int at, int left) {
+        if (a.dh) wy[c] = load_some(static_cast<const TW*>(a.pre) + at, left);
+        if (a.post) wb[c] = load_some(static_cast<const TW*>(a.post) + at, left);
+    };
+    const auto load_gate = [&](int c, int at, int left) {
+        if (a.gate) gate[c] = load_some(row_of<TB>(a.gate, group, hidden) + at, left);
+    };
+    float dpre[kRoomy ? kChunks : 1][8] = {}, dpost[kRoomy ? kChunks : 1][8] = {}, dgate[kChunks][8] = {};
+    __shared__ __attribute__((aligned(16))) float wide[2][kRoomy ? 1 : kTeam * kChunks * 8];
+    if constexpr (!kRoomy)
+        for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    s[0] += float(y[c][i]) * float(y[c][i]);
-                    s[1] += float(dh[c][i]) * float(w[i]) * float(y[c][i]);
+            for (int i = 0; i < 8; ++i) wide[0][(c * kTeam + t) * 8 + i] = wide[1][(c * kTeam + t) * 8 + i] = 0.f;
+    const auto add_wide = [&](int k, int c, const float(&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wide[k][(c * kTeam + t) * 8 + i] += v[i];
+    };
+    int64_t row = lo + team * run, in_run = 0;
+    Row r, next;
+    if constexpr (kRoomy) {
+        if (row < hi) {
+            load(r, row);
+            FSDP_CHUNKS(c, at, left) {
+                load_weights(c, at, left);
+                load_gate(c, at, left);
+            }
+        }
+    }
+    int flip = 0;
+    while (row < hi) {
+        const bool run_ends = ++in_run == run;
+        const int64_t after = row + 1 + (run_ends ? (kGroup - 1) * run : 0);
+        if constexpr (kRoomy) {
+            if (after < hi) load(next, after);
+        } else {
+            load(r, row);
+        }
+        float s[6] = {};             // sums of y^2, dh w y, branch^2, c dy, c dh w, c y
+        FSDP_CHUNKS(c, at, left) {
+            if constexpr (!kRoomy) {
+                load_weights(c, at, left);
+                load_gate(c, at, left);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float up = a.dh ? float(r.dh[c][i]) * float(wy[c][i]) : 0.f, y = a.dh ? float(r.y[c][i]) : 0.f;
+                s[0] += y * y;
+                s[1] += up * y;
+                if (a.post) {
+                    const float b = float(r.b[c][i]);
+                    const float k = b * float(wb[c][i]) * (a.gate ? float(gate[c][i]) : 1.f);
+                    s[2] += b * b;
+                    if (a.dy) s[3] += k * float(r.dy[c][i]);
+                    s[4] += k * up;
+                    s[5] += k * y;
                 }
             }
-            if (a.branch)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[2] += float(b[c][i]) * float(b[c][i]);
         }
         if (a.dh || a.post) {
-            group_sum<kTeam, 3>(s, part[flip]);
+            group_sum<kTeam, 6>(s, part[flip]);
             flip ^= 1;
         }
-        const float ry = rsqrtf(s[0] / float(hidden) + a.eps), my = ry * ry * ry * (s[1] / float(hidden));
-        const float rb = a.post ? rsqrtf(s[2] / float(hidden) + a.eps) : 1.f;
-        const TB* gate = a.gate ? row_of<TB>(a.gate, group, hidden) : nullptr;
-        float g[kChunks][8];                     // the gradient of y, then that of the normed branch times its weight
-        float dot[1] = {0.f};                    // the sum of dn * w * branch
+        const float per = 1.f / float(hidden);
+        const float ry = a.dh ? rsqrtf(s[0] * per + a.eps) : 0.f, my = ry * ry * ry * (s[1] * per);
+        const float rb = a.post ? rsqrtf(s[2] * per + a.eps) : 1.f;
+        const float mb = a.post ? rb * rb * rb * (a.branch_scale * (s[3] + ry * s[4] - my * s[5]) * per) : 0.f;
         FSDP_CHUNKS(c, at, left) {
+            if constexpr (!kRoomy) {
+                load_weights(c, at, left);
+                load_gate(c, at, left);
+            }
+            float g[8], term[8];     // the gradient of y, a row's term of a sum
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[c][i] = a.dy ? float(dy[c][i]) : 0.f;
-            if (a.dh) {
-                const Eight<TW> w = load_some(static_cast<const TW*>(a.pre) + at, left);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float up = float(dh[c][i]) * ry;
-                    dpre[c][i] += up * float(y[c][i]);
-                    g[c][i] += up * float(w[i]) - float(y[c][i]) * my;
+            for (int i = 0; i < 8; ++i) {
+                g[i] = a.dy ? float(r.dy[c][i]) : 0.f;
+                if (a.dh) {
+                    const float up = float(r.dh[c][i]) * ry, y = float(r.y[c][i]);
+                    if constexpr (kRoomy) dpre[c][i] += up * y;
+                    else term[i] = up * y;
+                    g[i] += up * float(wy[c][i]) - y * my;
                 }
             }
+            if constexpr (!kRoomy)
+                if (a.dh) add_wide(0, c, term);
             if (a.dx) {
                 float out[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) out[i] = a.residual_scale * g[c][i];
+                for (int i = 0; i < 8; ++i) out[i] = a.residual_scale * g[i];
                 store_some(row_of<TX>(a.dx, row, a.dx_stride) + at, left, out);
             }
             if (a.branch) {
-                Eight<TW> w;
-                Eight<TB> k;
-                if (a.post) w = load_some(static_cast<const TW*>(a.post) + at, left);
-                if (gate) k = load_some(gate + at, left);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float dn = a.branch_scale * g[c][i];
-                    const float n = float(b[c][i]) * rb;
-                    if (gate) {
-                        dgate[c][i] += dn * (a.post ? n * float(w[i]) : n);
-                        dn *= float(k[i]);
+                    float dn = a.branch_scale * g[i];
+                    const float b = float(r.b[c][i]), n = b * rb;
+                    if (a.gate) {
+                        dgate[c][i] += dn * (a.post ? n * float(wb[c][i]) : n);
+                        dn *= float(gate[c][i]);
                     }
                     if (a.post) {
-                        dpost[c][i] += dn * n;
-                        dn *= float(w[i]);
-                        dot[0] += dn * float(b[c][i]);
+                        if constexpr (kRoomy) dpost[c][i] += dn * n;
+                        else term[i] = dn * n;
+                        dn *= float(wb[c][i]);
                     }
-                    g[c][i] = dn;
+                    g[i] = rb * dn - b * mb;
                 }
+                if constexpr (!kRoomy)
+                    if (a.post) add_wide(1, c, term);
+                if (a.dbranch) store_some(row_of<TB>(a.dbranch, row, a.dbranch_stride) + at, left, g);
             }
         }
-        if (a.post) {
-            group_sum<kTeam, 1>(dot, part[flip]);
-            flip ^= 1;
-        }
-        if (a.branch) {
-            if (a.dbranch) {
-                const float mb = a.post ? rb * rb * rb * (dot[0] / float(hidden)) : 0.f;
-                FSDP_CHUNKS(c, at, left) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) g[c][i] = rb * g[c][i] - float(b[c][i]) * mb;
-                    store_some(row_of<TB>(a.dbranch, row, a.dbranch_stride) + at, left, g[c]);
-                }
-            }
-            if (a.gate && ++in_group == a.group_rows && a.units_per_group == 0) {
-                if (a.dgate) {
-                    TB* out = row_of<TB>(a.dgate, group, hidden);
-                    FSDP_CHUNKS(c, at, left) store_some(out + at, left, dgate[c]);
-                }
+        if (run_ends) {
+            in_run = 0;
+            if (a.gate && whole) {
+                if (a.dgate) FSDP_CHUNKS(c, at, left) store_some(row_of<TB>(a.dgate, group, hidden) + at, left, dgate[c]);
                 FSDP_CHUNKS(c, at, left)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dgate[c][i] = 0.f;
-                in_group = 0;
-                ++group;
+                group += kGroup;
+                if constexpr (kRoomy) {
+                    if (after < hi) FSDP_CHUNKS(c, at, left) load_gate(c, at, left);
+                }
             }
         }
+        row = after;
+        if constexpr (kRoomy) r = next;
     }
-    if (a.part_pre) FSDP_CHUNKS(c, at, left) store_some(a.part_pre + unit * hidden + at, left, dpre[c]);
-    if (a.part_post) FSDP_CHUNKS(c, at, left) store_some(a.part_post + unit * hidden + at, left, dpost[c]);
-    if (a.part_gate) FSDP_CHUNKS(c, at, left) store_some(a.part_gate + unit * hidden + at, left, dgate[c]);
+    const auto leave = [&](float* out, const float(&sum)[kChunks][8]) {
+        if (!out) return;
+        if constexpr (kGroup > 1) {
+            __syncthreads();         // `joined` has been read
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) joined[team][(c * kTeam + t) * 8 + i] = sum[c][i];
+            __syncthreads();
+            for (int j = threadIdx.x; j < hidden; j += kTeam * kGroup) {
+                float v = 0.f;
+#pragma unroll
+                for (int k = 0; k < kGroup; ++k) v += joined[k][j];
+                out[unit * hidden + j] = v;
+            }
+        } else {
+            FSDP_CHUNKS(c, at, left) store_some(out + unit * hidden + at, left, sum[c]);
+        }
+    };
+    if constexpr (kRoomy) {
+        leave(a.part_pre, dpre);
+        leave(a.part_post, dpost);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float* const out = k == 0 ? a.part_pre : a.part_post;
+            float sum[kChunks][8];
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[c][i] = wide[k][(c * kTeam + t) * 8 + i];
+            leave(out, sum);
+        }
+    }
+    leave(a.part_gate, dgate);
 }
 
 // ------------------------------------------------------------------ host side
@@ -274,15 +360,20 @@ fsdp_status with_types(fsdp_dtype stream, fsdp_dtype block, fsdp_dtype weight, F
     return block == FSDP_DTYPE_BF16 ? inner(bf16(0.f)) : block == FSDP_DTYPE_F16 ? inner(f16(0.f)) : inner(0.f);
 }
 
-// f(team, chunks): the smallest team that holds a row.
-template <typename F>
+// f(team, chunks) for a row.  kTwo: two chunks a thread in half the threads where
+// there is a choice (the forward of 16-bit blocks: 154 instead of 163 us at 8192 x
+// 8192, 85 instead of 111 at 8192 x 4097, where the larger team idles by half).
+template <bool kTwo, typename F>
 fsdp_status with_shape(int64_t hidden, F f) {
-    if (hidden <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    if (hidden <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    if (hidden <= 2048) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    if (hidden <= 4096) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
-    if (hidden <= 8192) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Chunks = std::integral_constant<int, kTwo ? 2 : 1>;
+    if (hidden <= 512) return f(std::integral_constant<int, 64>(), One());
+    if (hidden <= 1024) return f(std::integral_constant<int, 64>(), Two());
+    if (hidden <= 2048) return f(std::integral_constant<int, 256>(), One());
+    if (hidden <= 4096) return f(std::integral_constant<int, kTwo ? 256 : 512>(), Chunks());
+    if (hidden <= 8192) return f(std::integral_constant<int, kTwo ? 512 : 1024>(), Chunks());
+    return f(std::integral_constant<int, 1024>(), Two());
 }
 
 // The checks that the norms and their gradient share.
@@ -312,15 +403,20 @@ struct GradCut {
     int64_t bytes = 0;
 };
 
-int64_t units_wanted(int64_t hidden, int cus) {
-    const int64_t threads = hidden <= 1024 ? 64 : hidden <= 2048 ? 256 : hidden <= 4096 ? 512 : 1024;
-    return int64_t(cus) * (2048 / threads);
+// Workgroups per CU: more make more sums to join than they hide (twice as many: 6 %
+// slower at 8192 x 4096 and 8192 x 8192, 12 % at 16384 x 1024; half: 6 % slower at
+// 8192 x 4096, 16 % at 32768 x 256).  At least four rows to a unit for the same
+// reason, but for a few rows, which wait for each other.
+int64_t units_wanted(int64_t tokens, int64_t hidden, int cus) {
+    const int64_t per_cu = hidden <= 512 ? 4 : hidden <= 4096 ? 2 : 1;
+    const int64_t few = std::min(tokens, int64_t(cus) / 2);
+    return std::max<int64_t>(1, std::min(int64_t(cus) * per_cu, std::max(few, ceil_div(tokens, 4))));
 }
 
 GradCut cut_rows(const fsdp_norm_grad_args& a, int cus) {
     GradCut c;
     if (a.tokens > 0) {
-        const int64_t rows = ceil_div(a.tokens, units_wanted(a.hidden, cus));
+        const int64_t rows = ceil_div(a.tokens, units_wanted(a.tokens, a.hidden, cus));
         const int64_t group = a.gate ? a.tokens / a.gate_rows : 1;
         if (a.gate && group > rows) {
             c.units_per_group = ceil_div(group, rows);
@@ -400,7 +496,7 @@ extern "C" fsdp_status fsdp_block_norm(const fsdp_norm_args* args, hipStream_t s
                      a.h_stride, a.tokens, a.gate ? a.tokens / a.gate_rows : a.tokens, int(a.hidden), a.eps,
                      a.residual_scale, a.branch_scale};
     return with_types(a.stream_dtype, a.block_dtype, a.weight_dtype, [&](auto tx, auto tb, auto tw) {
-        return with_shape(a.hidden, [&](auto team, auto chunks) {
+        return with_shape<!std::is_same_v<decltype(tb), float>>(a.hidden, [&](auto team, auto chunks) {
             constexpr int kTeam = decltype(team)::value;
             const int64_t grid = std::min(kMaxGrid, ceil_div(a.tokens, kTeams<kTeam>));
             return launch(norm_kernel<decltype(tx), decltype(tb), decltype(tw), kTeam, decltype(chunks)::value>, k,
@@ -437,13 +533,13 @@ extern "C" fsdp_status fsdp_block_norm_grad(const fsdp_norm_grad_args* args, voi
         const NormGradArgs k{a.y, a.dy, a.dh, a.branch, a.post_weight, a.gate, a.pre_weight, a.dx, a.dbranch, a.dgate,
                              at(cut.pre), at(cut.post), at(cut.gate), a.y_stride, a.dy_stride, a.dh_stride,
                              a.branch_stride, a.dx_stride, a.dbranch_stride, a.tokens,
-                             a.gate ? a.tokens / a.gate_rows : a.tokens, cut.units, cut.unit_rows, cut.units_per_group,
+                             a.gate ? a.tokens / a.gate_rows : a.tokens, cut.unit_rows, cut.units_per_group,
                              int(a.hidden), a.eps, a.residual_scale, a.branch_scale};
         st = with_types(a.stream_dtype, a.block_dtype, a.weight_dtype, [&](auto tx, auto tb, auto tw) {
-            return with_shape(a.hidden, [&](auto team, auto chunks) {
+            return with_shape<false>(a.hidden, [&](auto team, auto chunks) {
                 constexpr int kTeam = decltype(team)::value;
                 return launch(norm_grad_kernel<decltype(tx), decltype(tb), decltype(tw), kTeam, decltype(chunks)::value>, k,
-                              dim3(unsigned(ceil_div(cut.units, kTeams<kTeam>))), kTeam * kTeams<kTeam>, stream);
+                              dim3(unsigned(cut.units)), kTeam * kTeams<kTeam>, stream);
             });
         });
         if (st != FSDP_OK) return st;
