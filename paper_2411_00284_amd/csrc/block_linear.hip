@@ -2,11 +2,10 @@
 // epilogue, and its gradient (include/fsdp_block.h).
 //
 // A product takes one of these forms:
-//   * product_kernel (block_product.h): 16-bit operands on the 16-byte grid, in
-//     tiles of 256 x 256, 128 x 128 or 64 x 128.  Operands off the grid are
+//   * product_kernel (block_product.h): operands on the 16-byte grid, in tiles of
+//     256 x 256 (16 bits only), 128 x 128 or 64 x 128.  Operands off the grid are
 //     laid on it by a copy into the workspace first.
-//   * row_kernel: at most four rows of x, 16-bit or fp32, at any address.
-//   * product_f32_kernel: fp32, at any address.
+//   * row_kernel: at most four rows of x, at any address.
 // With few tiles the sum over k is cut into parts, which join_parts_kernel joins
 // in order.
 
@@ -17,108 +16,6 @@
 
 namespace fsdp_block {
 namespace {
-
-// ------------------------------------------------------------------ fp32
-
-// A kTile x kTile tile of out in four waves, from operands of any alignment.
-// The fp32 matrix instructions run at a sixteenth of the bf16 rate, so the rest
-// needs no care: registers hold the next step while one is worked on in LDS.
-// A step is two 16-byte units of both operands per thread.
-template <int kTile>
-struct Step32 {
-    static constexpr int kDeep = 512 * 4 / kTile;      // k of a step: 16 or 32
-    static constexpr int kRow = kDeep + 4;             // floats of a row in LDS, padded by 16 bytes
-};
-
-// kColumns: the operand lies k-major, a unit is four rows at one k.
-template <int kTile, bool kColumns>
-__device__ __forceinline__ void load_f32(const float* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k1,
-                                         f32x4 (&out)[2]) {
-    constexpr int kDeep = Step32<kTile>::kDeep, kAcross = kColumns ? kTile / 4 : kDeep / 4;
-    struct __attribute__((packed, aligned(4))) any {
-        f32x4 v;
-    };
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int c = int(threadIdx.x) + 256 * u;
-        const int64_t i = first + (kColumns ? c % kAcross * 4 : c / kAcross);
-        const int64_t j = k0 + (kColumns ? c / kAcross : c % kAcross * 4);
-        const int64_t left = kColumns ? (j < k1 ? rows - i : 0) : (i < rows ? k1 - j : 0);
-        const float* at = kColumns ? p + j * stride + i : p + i * stride + j;
-        if (left >= 4) {
-            out[u] = reinterpret_cast<const any*>(at)->v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[u][e] = e < left ? at[e] : 0.f;
-        }
-    }
-}
-
-template <int kTile, bool kColumns>
-__device__ __forceinline__ void keep_f32(float* tile, const f32x4 (&in)[2]) {
-    constexpr int kRow = Step32<kTile>::kRow, kAcross = kColumns ? kTile / 4 : Step32<kTile>::kDeep / 4;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int c = int(threadIdx.x) + 256 * u;
-        if constexpr (kColumns) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) tile[(c % kAcross * 4 + e) * kRow + c / kAcross] = in[u][e];
-        } else {
-            *reinterpret_cast<f32x4*>(tile + c / kAcross * kRow + c % kAcross * 4) = in[u];
-        }
-    }
-}
-
-template <int kTile, bool kColumnsA, bool kColumnsB>
-__global__ __launch_bounds__(256) void product_f32_kernel(const Product p) {
-    constexpr int kDeep = Step32<kTile>::kDeep, kRow = Step32<kTile>::kRow, kN = kTile / 32;    // 16-row tiles of a wave
-    __shared__ __attribute__((aligned(16))) float ta[kTile * kRow], tb[kTile * kRow];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane % 16, q = lane / 16;
-    const int wi = wave / 2 * (kTile / 2), wj = wave % 2 * (kTile / 2);
-    const TilePlace t = tile_place(blockIdx.x, unsigned((p.m + kTile - 1) / kTile), unsigned((p.n + kTile - 1) / kTile),
-                                   unsigned(p.count));
-    const int64_t i0 = int64_t(t.row) * kTile, j0 = int64_t(t.column) * kTile;
-    const int64_t k0 = t.part * p.part_k, k1 = min(k0 + p.part_k, p.k);
-    const float* a = static_cast<const float*>(p.a);
-    const float* b = static_cast<const float*>(p.b);
-    f32x4 acc[kN][kN] = {};          // [A tile][B tile]
-    f32x4 ra[2], rb[2];
-    load_f32<kTile, kColumnsA>(a, p.a_stride, i0, p.m, k0, k1, ra);
-    load_f32<kTile, kColumnsB>(b, p.b_stride, j0, p.n, k0, k1, rb);
-    for (int64_t k = k0; k < k1; k += kDeep) {
-        __syncthreads();
-        keep_f32<kTile, kColumnsA>(ta, ra);
-        keep_f32<kTile, kColumnsB>(tb, rb);
-        __syncthreads();
-        if (k + kDeep < k1) {
-            load_f32<kTile, kColumnsA>(a, p.a_stride, i0, p.m, k + kDeep, k1, ra);
-            load_f32<kTile, kColumnsB>(b, p.b_stride, j0, p.n, k + kDeep, k1, rb);
-        }
-#pragma unroll
-        for (int s = 0; s < kDeep / 16; ++s) {
-            f32x4 fa[kN], fb[kN];
-#pragma unroll
-            for (int x = 0; x < kN; ++x) {
-                fa[x] = *reinterpret_cast<const f32x4*>(ta + (wi + 16 * x + r) * kRow + 16 * s + q * 4);
-                // Rows of B tiles are dealt so that a lane ends with eight neighbouring columns of two tiles.
-                fb[x] = *reinterpret_cast<const f32x4*>(tb + (wj + x / 2 * 32 + r / 4 * 8 + x % 2 * 4 + r % 4) * kRow + 16 * s + q * 4);
-            }
-#pragma unroll
-            for (int x = 0; x < kN; ++x)
-#pragma unroll
-                for (int y = 0; y < kN; ++y) acc[x][y] = mma(fb[y], fa[x], acc[x][y]);
-        }
-    }
-#pragma unroll
-    for (int x = 0; x < kN; ++x)
-#pragma unroll
-        for (int y = 0; y < kN; y += 2) {
-            float z[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) z[c] = acc[x][y + c / 4][c % 4];
-            leave8<float, kColumnsB>(p, t.part, i0 + wi + 16 * x + r, j0 + wj + y / 2 * 32 + q * 8, z);
-        }
-}
 
 // ------------------------------------------------------------------ few rows
 
@@ -170,11 +67,14 @@ __global__ __launch_bounds__(256) void row_kernel(const Product p) {
 
 // ------------------------------------------------------------------ onto the grid
 
-// Copies matrices to rows of whole 16-byte units, zeros after their columns.
+// Copies matrices to rows of whole lines, zeros after their columns up to a whole
+// 16-byte unit.  Sizes in halves of 32 bits, which fp32 elements are two of.  A
+// wave takes 64 units of a row, so that the division is one for all of them.
 struct PadArgs {
     const uint16_t* from[2];
     uint16_t* to[2];
-    int64_t rows[2], cols[2], stride[2], units[2];     // units: of a padded row
+    int64_t rows[2], cols[2], stride[2], to_stride[2];
+    uint32_t runs[2];                // of 64 units, in a row
 };
 
 __global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
@@ -182,12 +82,14 @@ __global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
     struct __attribute__((packed, aligned(2))) any {
         u16x8 v;
     };
-    const int64_t first = a.rows[0] * a.units[0], all = first + a.rows[1] * a.units[1];
-    for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < all; u += int64_t(gridDim.x) * 256) {
-        const int which = u >= first;
-        const int64_t unit = which ? u - first : u, row = unit / a.units[which], j = unit % a.units[which] * 8;
+    const uint32_t first = uint32_t(a.rows[0]) * a.runs[0], all = first + uint32_t(a.rows[1]) * a.runs[1];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
+    for (uint32_t item = wave; item < all; item += gridDim.x * 4) {
+        const int which = item >= first;
+        const uint32_t run = which ? item - first : item, row = run / a.runs[which];
+        const int64_t j = (int64_t(run - row * a.runs[which]) * 64 + threadIdx.x % 64) * 8, left = a.cols[which] - j;
+        if (left <= 0) continue;
         const uint16_t* at = a.from[which] + row * a.stride[which] + j;
-        const int64_t left = a.cols[which] - j;
         u16x8 v;
         if (left >= 8) {
             v = reinterpret_cast<const any*>(at)->v;
@@ -195,7 +97,7 @@ __global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = e < left ? at[e] : uint16_t(0);
         }
-        *reinterpret_cast<u16x8*>(a.to[which] + unit * 8) = v;
+        *reinterpret_cast<u16x8*>(a.to[which] + row * a.to_stride[which] + j) = v;
     }
 }
 
@@ -260,10 +162,10 @@ fsdp_status with_type(fsdp_dtype dtype, F f) {
     return dtype == FSDP_DTYPE_BF16 ? f(bf16(0.f)) : dtype == FSDP_DTYPE_F16 ? f(f16(0.f)) : f(0.f);
 }
 
-// The forms of a product in tiles.  Times in us of a step of 64 k (fp32: of 32)
-// on one MI355X: `alone` with one workgroup or few on a CU, `full` with every CU
-// holding `held` of them, and `fixed` for the start and the end of a tile, as
-// measured over products from 16 x 14336 x 4096 to 8192 x 28672 x 8192.
+// The forms of a product in tiles.  Times in us of a step (64 k, fp32: 32) on one
+// MI355X: `alone` with one workgroup on a CU, `full` with `held` of them on every
+// CU, and `fixed` for the start and the end of a tile, as measured over products
+// from 16 x 14336 x 4096 to 8192 x 28672 x 8192 (fp32: 2048 x 1024 x 688 and 4096^3).
 struct Form {
     int tile_m, tile_n, steps, held;
     double alone, full, fixed;
@@ -275,8 +177,8 @@ constexpr Form kForms16[] = {
     {64, 128, 4, 1, 0.25, 0.32, 3.5},
 };
 constexpr Form kForms32[] = {
-    {128, 128, 0, 2, 2.2, 4.0, 5.0},
-    {64, 64, 0, 4, 0.8, 2.0, 4.0},
+    {128, 128, 2, 2, 1.80, 3.60, 4.0},
+    {64, 128, 4, 1, 0.95, 0.95, 3.5},
 };
 
 // How one product is run.
@@ -332,21 +234,24 @@ Cut choose(const Shape& s, int cus) {
     return best;
 }
 
-struct Operand16 {
+struct Source {
     const void* p;
     int64_t rows, cols, stride;      // as it lies in memory
-    bool columns;
     bool zeros;                      // zeros follow a row, up to a whole 16-byte unit
 };
 
+// Elements of a row laid out in whole lines.
+int64_t lined(int64_t cols, fsdp_dtype dtype) { return round_up(cols, 128 / elem_bytes(dtype)); }
+
 // Whether an operand lies on the 16-byte grid in whole units, as product_kernel
-// reads it, with offsets of 64 rows or of a tile in 31 bits.
-bool on_grid(const Operand16& o) {
-    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % 8 == 0 && o.stride < (1 << 22) && (o.zeros || o.cols % 8 == 0);
+// reads it, with the offsets of a step in 31 bits.
+bool on_grid(const Source& o, fsdp_dtype dtype) {
+    const int unit = 16 / elem_bytes(dtype);
+    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % unit == 0 && o.stride < (1 << 21) && (o.zeros || o.cols % unit == 0);
 }
 
 // Adds a product's needs to those of `bytes`.
-Cut plan(const Shape& s, const Operand16& a, const Operand16& b, int cus, int64_t bytes) {
+Cut plan(const Shape& s, const Source& a, const Source& b, int cus, int64_t bytes) {
     Cut c = choose(s, cus);
     c.bytes = bytes;
     if (!c.form || s.m == 0 || s.n == 0 || s.k == 0) return c;
@@ -355,10 +260,9 @@ Cut plan(const Shape& s, const Operand16& a, const Operand16& b, int cus, int64_
         c.bytes += round_up(n, 256);
         return at;
     };
-    if (s.dtype != FSDP_DTYPE_F32) {
-        if (!on_grid(a)) c.pad_a = take(a.rows * round_up(a.cols, 8) * 2);
-        if (!on_grid(b)) c.pad_b = take(b.rows * round_up(b.cols, 8) * 2);
-    }
+    const int size = elem_bytes(s.dtype);
+    if (!on_grid(a, s.dtype)) c.pad_a = take(a.rows * lined(a.cols, s.dtype) * size);
+    if (!on_grid(b, s.dtype)) c.pad_b = take(b.rows * lined(b.cols, s.dtype) * size);
     if (c.count > 1) c.parts = take(int64_t(c.count) * s.m * round_up(s.n, 8) * 4);
     return c;
 }
@@ -368,8 +272,8 @@ fsdp_status launch_tiles(const Product& p, const Cut& c, fsdp_dtype dtype, hipSt
     const Form& f = *c.form;
     const dim3 grid(unsigned(ceil_div(p.m, f.tile_m) * ceil_div(p.n, f.tile_n) * c.count));
     if (dtype == FSDP_DTYPE_F32)
-        return f.tile_m == 128 ? launch(product_f32_kernel<128, kColumnsA, kColumnsB>, p, grid, 256, stream)
-                               : launch(product_f32_kernel<64, kColumnsA, kColumnsB>, p, grid, 256, stream);
+        return f.tile_m == 128 ? launch(product_kernel<float, kColumnsA, kColumnsB, 128, 128, 2>, p, grid, 256, stream)
+                               : launch(product_kernel<float, kColumnsA, kColumnsB, 64, 128, 4>, p, grid, 256, stream);
     const auto of = [&](auto type) {
         using T = decltype(type);
         if (f.tile_m == 256) return launch(product_kernel<T, kColumnsA, kColumnsB, 256, 256, 2>, p, grid, 256, stream);
@@ -381,7 +285,7 @@ fsdp_status launch_tiles(const Product& p, const Cut& c, fsdp_dtype dtype, hipSt
 }
 
 // One product, as `c` says.
-fsdp_status run_product(const Shape& s, const Operand16& a, const Operand16& b, const Epilogue& e, const Cut& c, char* ws,
+fsdp_status run_product(const Shape& s, const Source& a, const Source& b, const Epilogue& e, const Cut& c, char* ws,
                         hipStream_t stream) {
     if (s.m == 0 || s.n == 0) return FSDP_OK;
     Product p{a.p, b.p, a.stride, b.stride, s.m, s.n, s.k, e, nullptr, s.k, 1};
@@ -397,22 +301,25 @@ fsdp_status run_product(const Shape& s, const Operand16& a, const Operand16& b, 
     fsdp_status st;
     if (c.pad_a >= 0 || c.pad_b >= 0) {
         PadArgs pad{};
-        const auto lay = [&](int which, const Operand16& o, int64_t at, const void** to, int64_t* stride) {
-            pad.units[which] = 1;
+        const int halves = elem_bytes(s.dtype) / 2;
+        const auto lay = [&](int which, const Source& o, int64_t at, const void** to, int64_t* stride) {
+            pad.runs[which] = 1;
             if (at < 0) return;
             pad.from[which] = static_cast<const uint16_t*>(o.p);
             pad.to[which] = reinterpret_cast<uint16_t*>(ws + at);
             pad.rows[which] = o.rows;
-            pad.cols[which] = o.cols;
-            pad.stride[which] = o.stride;
-            pad.units[which] = ceil_div(o.cols, 8);
+            pad.cols[which] = o.cols * halves;
+            pad.stride[which] = o.stride * halves;
+            pad.to_stride[which] = lined(o.cols, s.dtype) * halves;
+            pad.runs[which] = uint32_t(ceil_div(pad.cols[which], 512));
             *to = ws + at;
-            *stride = pad.units[which] * 8;
+            *stride = lined(o.cols, s.dtype);
         };
         lay(0, a, c.pad_a, &p.a, &p.a_stride);
         lay(1, b, c.pad_b, &p.b, &p.b_stride);
-        const int64_t units = pad.rows[0] * pad.units[0] + pad.rows[1] * pad.units[1];
-        if ((st = launch(pad_kernel, pad, dim3(unsigned(std::min<int64_t>(ceil_div(units, 256), 1 << 16))), 256, stream)) != FSDP_OK)
+        const int64_t runs = pad.rows[0] * pad.runs[0] + pad.rows[1] * pad.runs[1];
+        // check_sizes bounds rows x cols by 2^34 and rows by 2^28: the runs fit 31 bits.
+        if ((st = launch(pad_kernel, pad, dim3(unsigned(std::min<int64_t>(ceil_div(runs, 4), 1 << 16))), 256, stream)) != FSDP_OK)
             return st;
     }
     p.part_k = c.part_k;
@@ -476,8 +383,8 @@ int64_t row_stride(int64_t rows, int64_t cols, int64_t stride) { return rows > 1
 
 // The operands of the three products.
 Shape forward_shape(const fsdp_linear_args& a) { return {a.m, a.n, a.k, a.dtype, false, false}; }
-Operand16 forward_x(const fsdp_linear_args& a) { return {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false, false}; }
-Operand16 forward_w(const fsdp_linear_args& a) { return {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false, false}; }
+Source forward_x(const fsdp_linear_args& a) { return {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false}; }
+Source forward_w(const fsdp_linear_args& a) { return {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false}; }
 
 // What a gradient needs besides its outputs.
 struct GradParts {
@@ -486,7 +393,7 @@ struct GradParts {
     int64_t dz = -1, dbias = -1;     // byte offsets
     int64_t bytes = 0;               // of the workspace
     Shape dx_shape, dw_shape;
-    Operand16 dz_rows, weight, dz_columns, x;
+    Source from_dz, weight, x;
     Cut dx, dw;
 };
 
@@ -499,7 +406,7 @@ GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
         g.parts = ceil_div(a.m, g.part_rows);
         if (g.slopes && (a.dx || a.dweight)) {
             g.dz = g.bytes;
-            g.bytes += round_up(a.m * round_up(a.n, 8) * elem_bytes(a.dtype), 256);
+            g.bytes += round_up(a.m * lined(a.n, a.dtype) * elem_bytes(a.dtype), 256);
         }
         if (a.dbias) {
             g.dbias = g.bytes;
@@ -507,21 +414,20 @@ GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
         }
     }
     const void* const dz = g.dz >= 0 ? ws + g.dz : a.dout;
-    const int64_t stride = g.dz >= 0 ? round_up(a.n, 8) : row_stride(a.m, a.n, a.dout_stride);
-    g.dz_rows = {dz, a.m, a.n, stride, false, g.dz >= 0};
-    g.dz_columns = {dz, a.m, a.n, stride, true, g.dz >= 0};
-    g.weight = {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), true, false};
-    g.x = {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), true, false};
+    const int64_t stride = g.dz >= 0 ? lined(a.n, a.dtype) : row_stride(a.m, a.n, a.dout_stride);
+    g.from_dz = {dz, a.m, a.n, stride, g.dz >= 0};
+    g.weight = {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false};
+    g.x = {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false};
     g.dx_shape = {a.m, a.k, a.n, a.dtype, false, true};
     g.dw_shape = {a.n, a.k, a.m, a.dtype, true, true};
     const int64_t own = g.bytes;
     // The two products follow each other on the stream: they share what they need.
     if (a.dx) {
-        g.dx = plan(g.dx_shape, g.dz_rows, g.weight, cus, own);
+        g.dx = plan(g.dx_shape, g.from_dz, g.weight, cus, own);
         g.bytes = std::max(g.bytes, g.dx.bytes);
     }
     if (a.dweight) {
-        g.dw = plan(g.dw_shape, g.dz_columns, g.x, cus, own);
+        g.dw = plan(g.dw_shape, g.from_dz, g.x, cus, own);
         g.bytes = std::max(g.bytes, g.dw.bytes);
     }
     return g;
@@ -553,7 +459,7 @@ extern "C" fsdp_status fsdp_block_linear(const fsdp_linear_args* args, void* wor
     const int cus = cu_count(&st);
     if (cus == 0) return st;
     const Shape s = forward_shape(a);
-    const Operand16 x = forward_x(a), w = forward_w(a);
+    const Source x = forward_x(a), w = forward_w(a);
     const Cut c = plan(s, x, w, cus, 0);
     if ((st = check_workspace(workspace, workspace_bytes, c.bytes)) != FSDP_OK) return st;
     const Epilogue e{a.bias, a.times, a.residual, a.pre, a.out, a.times_stride, a.residual_stride, a.pre_stride, a.out_stride,
@@ -587,7 +493,7 @@ extern "C" fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args,
     float* const part = g.dbias < 0 ? nullptr : reinterpret_cast<float*>(ws + g.dbias);
     if (a.m > 0 && a.n > 0 && (g.dz >= 0 || part || a.dtimes)) {
         const SlopeArgs s{a.dout, a.pre, a.times, g.dz >= 0 ? ws + g.dz : nullptr, a.dtimes, part, a.dout_stride,
-                          a.pre_stride, a.times_stride, g.dz_rows.stride, a.dtimes_stride, a.m, a.n, g.part_rows, a.activation};
+                          a.pre_stride, a.times_stride, g.from_dz.stride, a.dtimes_stride, a.m, a.n, g.part_rows, a.activation};
         const dim3 grid(unsigned(ceil_div(a.n, 512)), unsigned(g.parts));
         st = with_type(a.dtype, [&](auto type) { return launch(slope_kernel<decltype(type)>, s, grid, 256, stream); });
         if (st != FSDP_OK) return st;
@@ -599,9 +505,9 @@ extern "C" fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args,
         return Epilogue{nullptr, nullptr, nullptr, nullptr, out, 0, 0, 0, stride, FSDP_ACT_NONE};
     };
     if (a.dx) {
-        st = run_product(g.dx_shape, g.dz_rows, g.weight, plain(a.dx, a.dx_stride), g.dx, ws, stream);
+        st = run_product(g.dx_shape, g.from_dz, g.weight, plain(a.dx, a.dx_stride), g.dx, ws, stream);
         if (st != FSDP_OK) return st;
     }
-    if (a.dweight) st = run_product(g.dw_shape, g.dz_columns, g.x, plain(a.dweight, a.dweight_stride), g.dw, ws, stream);
+    if (a.dweight) st = run_product(g.dw_shape, g.from_dz, g.x, plain(a.dweight, a.dweight_stride), g.dw, ws, stream);
     return st;
 }

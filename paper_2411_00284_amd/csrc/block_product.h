@@ -1,5 +1,5 @@
-// The matrix product of 16-bit operands on the 16-byte grid, its epilogue, and
-// what else the product kernels share.
+// The matrix product of operands on the 16-byte grid, its epilogue, and what else
+// the product kernels share.
 //
 // All products of a linear layer (x W^T, dz W, dz^T x) are
 // out[i][j] = sum_k A[i][k] B[j][k]; an operand lies row by row (k contiguous:
@@ -138,12 +138,11 @@ __device__ __forceinline__ f32x16 mma(Eight<bf16> a, Eight<bf16> b, f32x16 c) {
 __device__ __forceinline__ f32x16 mma(Eight<f16> a, Eight<f16> b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-// 16 bytes of fp32 of A rows and of B rows per lane -> a 16 x 16 tile.  Lane l
-// holds row l % 16 of both and the (l / 16)-th 16 bytes of a 64-byte run of k;
-// element r of lane l of the tile is at A row 4 (l / 16) + r, B row l % 16.
-__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+// fp32, two k an instruction: a lane's four values are four of them, the same
+// for both operands.  A sixteenth of the 16-bit rate.
+__device__ __forceinline__ f32x16 mma(f32x4 a, f32x4 b, f32x16 c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
     return c;
 }
 
@@ -169,8 +168,8 @@ __device__ __forceinline__ TilePlace tile_place(unsigned id, unsigned tiles_m, u
 
 // A kTileM x kTileN tile of out in four waves, each a quarter of it.
 //
-// k goes by in steps of 64: 128 bytes of a row, a cache line (with steps of half
-// a line the L2 answers twice the requests: 1170 instead of 1300 TFLOP/s at
+// k goes by in steps of 128 bytes of a row, a cache line: 64 k of 16 bits, 32 of
+// fp32 (with steps of half a line the L2 answers twice the requests: 1170 instead of 1300 TFLOP/s at
 // 8192 x 8192 x 8192).  kSteps steps of both operands lie in LDS.  A step is
 // worked on in two halves, two matrix instructions deep each, whose operands lie
 // in registers: while the matrix cores take one half the registers of the next
@@ -182,13 +181,17 @@ __device__ __forceinline__ TilePlace tile_place(unsigned id, unsigned tiles_m, u
 //
 // LDS layout, for conflict-free reads: "rows" 128 bytes per row, with the
 // 16-byte units of row r exchanged by r / 2; "columns" one run of columns per k,
-// its pairs of 32-byte blocks exchanged by k, read with the transposing load.
-template <int kRows, bool kColumns>
+// its units exchanged by k, read with the transposing load or (fp32) by element.
+template <typename T, int kRows, bool kColumns>
 struct Operand {
+    static constexpr int kSize = int(sizeof(T)), kDeep = 128 / kSize, kUnit = 16 / kSize;   // k of a step, elements of a unit
     static constexpr int kBytes = kRows * 128;         // of a step
     static constexpr int kLoads = kRows / 32;          // per thread and step, 16 bytes each
-    static constexpr int kUnits = kRows / 8;           // 16-byte units of one k of "columns"
-    __device__ static __forceinline__ int exchange(int k) { return kRows >= 128 ? (k & 3) * 2 : k & 2; }
+    static constexpr int kUnits = kRows / kUnit;       // units of one k of "columns"
+    // What the units of k are exchanged by.
+    __device__ static __forceinline__ int exchange(int k) {
+        return kSize == 4 ? (k >> 2 & 1) * 8 : kRows >= 128 ? (k & 3) * 4 : (k & 2) * 2;
+    }
 
     const char* at;            // the step's first byte
     int64_t step;              // bytes from a step to the next
@@ -199,24 +202,25 @@ struct Operand {
     __device__ __forceinline__ Operand(const void* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k1) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         if constexpr (kColumns) {
-            at = static_cast<const char*>(p) + (k0 * stride + first) * 2;
-            step = 64 * stride * 2;
-            left = (k1 - 1 - k0) * stride * 2 + (rows - first + 7) / 8 * 16;
+            at = static_cast<const char*>(p) + (k0 * stride + first) * kSize;
+            step = kDeep * stride * kSize;
+            left = (k1 - 1 - k0) * stride * kSize + (rows - first + kUnit - 1) / kUnit * 16;
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int unit = (j * 4 + wave) * 64 + lane, kk = unit / kUnits, u = unit % kUnits;
-                offset[j] = uint32_t(kk * stride * 2 + ((u / 2 ^ exchange(kk)) * 2 + u % 2) * 16);
+                offset[j] = uint32_t(kk * stride * kSize + (u ^ exchange(kk)) * 16);
             }
             k = 0;
         } else {
-            at = static_cast<const char*>(p) + (first * stride + k0) * 2;
+            at = static_cast<const char*>(p) + (first * stride + k0) * kSize;
             step = 128;
-            left = (rows - 1 - first) * stride * 2 + (k1 - k0 + 7) / 8 * 16;
-            k = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
+            left = (rows - 1 - first) * stride * kSize + (k1 - k0 + kUnit - 1) / kUnit * 16;
+            const int u = lane % 8 ^ (wave % 2 * 4 + lane / 16);
+            k = u * kUnit;
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int row = (j * 4 + wave) * 8 + lane / 8;
-                offset[j] = uint32_t(row * stride * 2 + k * 2);
+                offset[j] = uint32_t(row * stride * kSize + u * 16);
             }
         }
     }
@@ -237,22 +241,32 @@ struct Operand {
     }
 };
 
-// A wave's registers of half a step: kTiles times 32 rows of an operand, for
-// two matrix instructions each.
+// The 16 bytes of an operand that a lane gives to a matrix instruction.
+template <typename T>
+struct LaneUnit {
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
+// A wave's registers of half a step: kTiles times 32 rows of an operand, in two
+// pairs of units.
 template <typename T, int kRows, bool kColumns, int kTiles>
 struct Fragments {
+    static constexpr bool kWide = sizeof(T) == 4;
     static constexpr int kPlaces = kColumns ? kTiles : 4;
-    Eight<T> v[2][kTiles];
+    static constexpr int kReads = 2 * kTiles * (!kColumns ? 1 : kWide ? 4 : 2);     // LDS instructions
+    typename LaneUnit<T>::type v[2][kTiles];
     // This lane's places in a step's LDS, of the wave whose first row is `first`.
     __device__ static __forceinline__ void lane_places(int first, int (&place)[kPlaces]) {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int x = 0; x < kPlaces; ++x) {
-            if constexpr (kColumns) {
-                const int k = lane / 32 * 8 + lane % 16 / 4, block = first / 16 + 2 * x + lane / 16 % 2;
-                place[x] = k * kRows * 2 + (block ^ Operand<kRows, true>::exchange(k)) * 32 + lane % 4 * 8;
-            } else {
+            if constexpr (!kColumns) {
                 place[x] = (first + lane % 32) * 128 + ((2 * x + lane / 32) ^ lane / 2 % 8) * 16;
+            } else {
+                // 16 bits: the 4 x 16 block of k and columns that 16 lanes point to; fp32: a column of four k.
+                const int k = kWide ? lane / 32 * 4 : lane / 32 * 8 + lane % 16 / 4;
+                const int byte = kWide ? (first + 32 * x + lane % 32) * 4 : (first + 32 * x + lane / 16 % 2 * 16 + lane % 4 * 4) * 2;
+                place[x] = k * kRows * int(sizeof(T)) + (byte ^ Operand<T, kRows, true>::exchange(k) * 16);
             }
         }
     }
@@ -263,14 +277,18 @@ struct Fragments {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int x = 0; x < kTiles; ++x) {
-                if constexpr (kColumns) {
-                    // The transposing load gives lane i of 16 the i-th column of the 4 x 16 block that the 16 lanes point to.
+                if constexpr (!kColumns) {
+                    v[h][x] = *reinterpret_cast<const typename LaneUnit<T>::type*>(lds + place[2 * half + h] + x * 32 * 128);
+                } else if constexpr (kWide) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        v[h][x][i] = *reinterpret_cast<const float*>(lds + place[x] + ((2 * half + h) * 8 + i) * kRows * 4);
+                } else {
+                    // The transposing load gives lane i of 16 the i-th column of their block.
                     const char* const at = lds + place[x] + (2 * half + h) * 16 * kRows * 2;
                     v[h][x] = __builtin_bit_cast(Eight<T>, __builtin_shufflevector(
                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at),
                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRows * 2)), 0, 1, 2, 3, 4, 5, 6, 7));
-                } else {
-                    v[h][x] = *reinterpret_cast<const Eight<T>*>(lds + place[2 * half + h] + x * 32 * 128);
                 }
             }
     }
@@ -278,8 +296,9 @@ struct Fragments {
 
 template <typename T, bool kColumnsA, bool kColumnsB, int kTileM, int kTileN, int kSteps>
 __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void product_kernel(const Product p) {
-    using A = Operand<kTileM, kColumnsA>;
-    using B = Operand<kTileN, kColumnsB>;
+    using A = Operand<T, kTileM, kColumnsA>;
+    using B = Operand<T, kTileN, kColumnsB>;
+    constexpr int kDeep = A::kDeep;
     constexpr int kA = kTileM / 64, kB = kTileN / 64;            // 32-row tiles of a wave
     // One array per step: their reads and loads are known not to touch each other.
     __shared__ __attribute__((aligned(1024))) char a0[A::kBytes], a1[A::kBytes], a2[kSteps > 2 ? A::kBytes : 16],
@@ -317,9 +336,9 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     const auto ask = [&](char* la, char* lb) {
         a.load(la, rest);
         b.load(lb, rest);
-        rest -= 64;
+        rest -= kDeep;
     };
-    constexpr int kMma = 2 * kA * kB, kReads = 2 * kA * (kColumnsA ? 2 : 1) + 2 * kB * (kColumnsB ? 2 : 1),
+    constexpr int kMma = 2 * kA * kB * (sizeof(T) == 4 ? 4 : 1), kReads = FA::kReads + FB::kReads,
                   kLoads = A::kLoads + B::kLoads;
     // Half a step: the order of issue is LDS reads first, under the matrix
     // instructions, which then have the rest of the half to arrive; the memory
@@ -370,7 +389,7 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     fa[0].read(a0, pa, 0);
     fb[0].read(b0, pb, 0);
     // Steps past the end add zeros: the loop takes kSteps at a time.
-    for (int64_t left = k1 - k0; left > 0; left -= 64 * kSteps) {
+    for (int64_t left = k1 - k0; left > 0; left -= kDeep * kSteps) {
         step(a0, b0, a1, b1);
         if constexpr (kSteps == 2) {
             step(a1, b1, a0, b0);
