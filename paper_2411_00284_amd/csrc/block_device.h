@@ -30,6 +30,12 @@ template <typename T>
 __device__ __forceinline__ Eight<T> load8(const T* p) {
     return reinterpret_cast<const typename Vec8<T>::any*>(p)->v;
 }
+// The same of what is read once: past the caches.
+template <typename T>
+__device__ __forceinline__ Eight<T> load8_once(const T* p) {
+    typedef Eight<T> any __attribute__((aligned(sizeof(T))));
+    return __builtin_nontemporal_load(reinterpret_cast<const any*>(p));
+}
 template <typename T>
 __device__ __forceinline__ void store8(T* p, Eight<T> v) {
     reinterpret_cast<typename Vec8<T>::any*>(p)->v = v;

@@ -20,49 +20,52 @@ namespace {
 // ------------------------------------------------------------------ few rows
 
 // x W^T of at most kRows rows of x: a wave takes kOut rows of W, eight elements
-// per lane at a time, and reads W once; x comes from cache.  Bound by reading W.
-constexpr int kRowOut = 2;
+// per lane at a time, and reads W once, past the caches (16 bits: 22.6 instead of
+// 24.4 us at 1 x 14336 x 4096, 5.2 TB/s; fp32 elements are half a line a load and
+// stay); x comes from cache, the more of it per row of W the more rows there are.
+template <typename T, int kRows>
+constexpr int kRowOut = kRows > 2 ? 4 : 2;
 
 template <typename T, int kRows>
 __global__ __launch_bounds__(256) void row_kernel(const Product p) {
+    constexpr int kOut = kRowOut<T, kRows>;
     const int lane = threadIdx.x & 63;
-    const int64_t j0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * kRowOut;
+    const int64_t j0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * kOut;
     if (j0 >= p.n) return;
-    const T* w[kRowOut];
+    const T* w[kOut];
 #pragma unroll
-    for (int o = 0; o < kRowOut; ++o) w[o] = static_cast<const T*>(p.b) + min(j0 + o, p.n - 1) * p.b_stride;
+    for (int o = 0; o < kOut; ++o) w[o] = static_cast<const T*>(p.b) + min(j0 + o, p.n - 1) * p.b_stride;
     const T* x = static_cast<const T*>(p.a);
-    float sum[kRowOut][kRows] = {};
+    float sum[kOut][kRows] = {};
     const auto add = [&](int64_t k, int n) {
-        Eight<T> v[kRowOut];
+        Eight<T> v[kOut];
 #pragma unroll
-        for (int o = 0; o < kRowOut; ++o) v[o] = load_some(w[o] + k, n);
+        for (int o = 0; o < kOut; ++o) v[o] = n == 8 && sizeof(T) == 2 ? load8_once(w[o] + k) : load_some(w[o] + k, n);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             const Eight<T> u = load_some(x + min(int64_t(i), p.m - 1) * p.a_stride + k, n);
 #pragma unroll
-            for (int o = 0; o < kRowOut; ++o)
+            for (int o = 0; o < kOut; ++o)
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sum[o][i] += float(v[o][c]) * float(u[c]);
         }
     };
     int64_t k = lane * 8;
-#pragma unroll 4
+#pragma unroll(8 / kOut)
     for (; k + 8 <= p.k; k += 512) add(k, 8);
     if (k < p.k) add(k, int(p.k - k));
 #pragma unroll
-    for (int o = 0; o < kRowOut; ++o)
+    for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int i = 0; i < kRows; ++i) sum[o][i] = wave_sum(sum[o][i]);
-    if (lane < p.m)
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
-            if (lane == i)
+    for (int i = 0; i < kRows; ++i)
+        if (lane == i && lane < p.m)
 #pragma unroll
-                for (int o = 0; o < kRowOut; ++o) {
-                    float z[8] = {sum[o][i]};
-                    if (j0 + o < p.n) finish8<T>(p.e, i, j0 + o, 1, z);
-                }
+            for (int o = 0; o < kOut; ++o) {
+                float z[8] = {sum[o][i]};
+                if (j0 + o < p.n) finish8<T>(p.e, i, j0 + o, 1, z);
+            }
 }
 
 // ------------------------------------------------------------------ onto the grid
@@ -164,8 +167,8 @@ fsdp_status with_type(fsdp_dtype dtype, F f) {
 
 // The forms of a product in tiles.  Times in us of a step (64 k, fp32: 32) on one
 // MI355X: `alone` with one workgroup on a CU, `full` with `held` of them on every
-// CU, and `fixed` for the start and the end of a tile, as measured over products
-// from 16 x 14336 x 4096 to 8192 x 28672 x 8192 (fp32: 2048 x 1024 x 688 and 4096^3).
+// CU, and `fixed` for the start and the end of a tile, as measured over products from
+// 16 x 14336 x 4096 to 8192 x 28672 x 8192 (fp32: 2048 x 1024 x 688 and 4096^3).
 struct Form {
     int tile_m, tile_n, steps, held;
     double alone, full, fixed;
@@ -199,10 +202,10 @@ struct Shape {
 constexpr int64_t kMostRows = 4;     // of row_kernel
 
 // The form and the cut with the least expected time: whole rounds of workgroups
-// over the CUs, what is left of the last round, reading the operands at 5.5 TB/s
+// over the CUs, the fullest CU of the last round, reading the operands at 5.5 TB/s
 // if that takes longer, and the join of the parts (3 us, and 8 bytes moved per
-// value and part).  From at most four rows of x on, row_kernel reads the weight
-// at HBM's rate in one launch.
+// value and part).  Up to four rows of x, row_kernel reads the weight at HBM's
+// rate in one launch.
 Cut choose(const Shape& s, int cus) {
     Cut best;
     if (s.m <= kMostRows && !s.columns_a && !s.columns_b) return best;
@@ -210,24 +213,27 @@ Cut choose(const Shape& s, int cus) {
     const Form* const forms = wide ? kForms32 : kForms16;
     const int step_k = wide ? 32 : 64;
     const int64_t steps = std::max<int64_t>(1, ceil_div(s.k, step_k));
-    const double bytes = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k));
+    const double reading = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k)) / 5.5e6;
+    const double joining = double(s.m) * double(s.n) * 8 / 5e6;
     double least = 0;
     for (int f = 0; f < (wide ? 2 : 4); ++f) {
         const Form& form = forms[f];
-        const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n);
-        for (int64_t parts : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (parts > 1 && (steps < 4 * parts || tiles * (parts - 1) > 4 * int64_t(cus))) break;
-            const int64_t each = ceil_div(steps, parts), groups = tiles * ceil_div(steps, each);
-            const int64_t slots = int64_t(cus) * form.held, whole = groups / slots, rest = groups % slots;
+        const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n), slots = int64_t(cus) * form.held;
+        for (int parts = 1; parts <= 16; ++parts) {
+            // Parts of at least four steps, and no more of them than some rounds.
+            if (parts > 1 && (steps < 4 * parts || tiles * (parts - 1) > 3 * int64_t(cus))) break;
+            const int64_t each = (steps + parts - 1) / parts, count = (steps + each - 1) / each;
+            if (count != parts) continue;
+            const int64_t groups = tiles * parts, whole = groups / slots, rest = groups - whole * slots;
             double time = double(whole) * (double(each) * form.full + form.fixed);
-            if (rest) time += double(each) * std::max(form.alone, form.full * double(rest) / double(slots)) + form.fixed;
-            time = std::max(time, bytes / 5.5e6 + form.fixed);
-            if (parts > 1) time += 3.0 + double(parts) * double(s.m) * double(s.n) * 8 / 5e6;
+            if (rest) time += double(each) * (rest > cus ? form.full : form.alone) + form.fixed;
+            time = std::max(time, reading + form.fixed);
+            if (parts > 1) time += 3.0 + double(parts) * joining;
             if (!best.form || time < least) {
                 least = time;
                 best.form = &form;
                 best.part_k = each * step_k;
-                best.count = int(ceil_div(steps, each));
+                best.count = parts;
             }
         }
     }
@@ -290,12 +296,16 @@ fsdp_status run_product(const Shape& s, const Source& a, const Source& b, const 
     if (s.m == 0 || s.n == 0) return FSDP_OK;
     Product p{a.p, b.p, a.stride, b.stride, s.m, s.n, s.k, e, nullptr, s.k, 1};
     if (!c.form) {
-        const dim3 grid(unsigned(ceil_div(s.n, 4 * kRowOut)));
         return with_type(s.dtype, [&](auto type) {
             using T = decltype(type);
-            return s.m == 1   ? launch(row_kernel<T, 1>, p, grid, 256, stream)
-                   : s.m == 2 ? launch(row_kernel<T, 2>, p, grid, 256, stream)
-                              : launch(row_kernel<T, 4>, p, grid, 256, stream);
+            const auto rows = [&](auto count) {
+                constexpr int kRows = decltype(count)::value;
+                const dim3 grid(unsigned(ceil_div(s.n, 4 * kRowOut<T, kRows>)));
+                return launch(row_kernel<T, kRows>, p, grid, 256, stream);
+            };
+            return s.m == 1   ? rows(std::integral_constant<int, 1>())
+                   : s.m == 2 ? rows(std::integral_constant<int, 2>())
+                              : rows(std::integral_constant<int, 4>());
         });
     }
     fsdp_status st;
