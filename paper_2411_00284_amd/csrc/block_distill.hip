@@ -160,7 +160,7 @@ __device__ __forceinline__ void for_same_ids(int top, const int* ids, const floa
 // kHeld units per thread stay in registers; those of the first group are asked
 // for before the teacher's entries are looked at.
 template <typename T, int kThreads, int kHeld>
-__global__ __launch_bounds__(kThreads, 4) void distill_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(const DistillArgs a) {
     constexpr int kWaves = kThreads / 64, n = Unit<T>::n;
     static_assert(kHeld >= 4 && kHeld % 2 == 0);
     __shared__ float p[FSDP_DISTILL_MAX_TOP], picked[FSDP_DISTILL_MAX_TOP];
@@ -195,7 +195,8 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(const DistillArgs 
         top = __any(top != top) ? NAN : wave_max(top);
         if (lane == 0) wm[wave] = top;
         bad = __syncthreads_or(bad);
-        for (int w = 0; w < kWaves; ++w) top = wm[w] != wm[w] || top != top ? NAN : fmaxf(top, wm[w]);
+        top = wm[lane % kWaves];                                // over the waves, as over a wave's lanes
+        top = __any(top != top) ? NAN : wave_max(top);
         if (top == -INFINITY || bad) {                          // no entry with any mass, or one out of range
             const float fill = bad ? NAN : 0.f;
             if (t == 0 && a.loss) a.loss[row] = fill;
@@ -239,11 +240,11 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(const DistillArgs 
             ws[wave] = x.s;
         }
         __syncthreads();
-        x = Softmax();
-        sum = 0.f;
-        for (int w = 0; w < kWaves; ++w) {
-            sum += wt[w];
-            if (!a.lse_in) x.join(wm[w], ws[w], c);
+        sum = wave_sum(lane < kWaves ? wt[lane] : 0.f);
+        if (!a.lse_in) {
+            const float m = wm[lane % kWaves], s1 = lane < kWaves ? ws[lane] : 0.f;
+            x.m = wave_max(m);
+            x.s = wave_sum(s1 == 0.f ? 0.f : s1 * exp2_fast(Softmax::shift(m, c) - Softmax::shift(x.m, c)));
         }
         const double teacher = a.teacher_lse ? double(a.teacher_lse[row]) : double(top) * per_tau + log2_of(sum) * ln2;
         // The rounding of m c, which the sum's terms had, is taken out of its logarithm.
@@ -271,14 +272,14 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(const DistillArgs 
             wd[wave] = loss;
         }
         __syncthreads();
-        if (t == 0 && a.loss) {
-            loss = 0.0;
-            for (int w = 0; w < kWaves; ++w) loss += wd[w];
-            a.loss[row] = float(tau * tau * loss);
+        if (wave == 0 && a.loss) {
+            loss = lane < kWaves ? wd[lane] : 0.0;
+#pragma unroll
+            for (int d = kWaves / 2; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+            if (t == 0) a.loss[row] = float(tau * tau * loss);
         }
         if (a.dlogits) {
-            mass = 0.f;
-            for (int w = 0; w < kWaves; ++w) mass += wp[w];
+            mass = wave_sum(lane < kWaves ? wp[lane] : 0.f);
             // q = 2^(s c - b): b in two parts, the second as a factor
             const double b = lse * tau * double(c);
             const float base = float(b), scale = weight * a.tau;
@@ -347,18 +348,19 @@ fsdp_status run(const fsdp_distill_args* args, bool backward, hipStream_t stream
     fsdp_status found = FSDP_OK;
     const int cus = cu_count(&found);
     if (cus == 0) return found;
-    // Few rows: as many threads as a workgroup has, each with more of the row on
-    // its way at once.  Else 256 threads, the most workgroups that a row's chain of
-    // loads and sums can hide behind; for a row that is read twice and long, 512,
-    // which hold twice of it (at 4096 x 128256 in bf16, loss and gradient: 445
-    // instead of 488 us; the loss alone 210 instead of 191, and at 8192 x 32000 both
-    // 247 instead of 224).
+    // Rows that 256 threads hold in four units each: the fewest steps from one
+    // wave to the next.  Few rows: as many threads as a workgroup has, each with
+    // more of the row on its way at once.  Else 256 threads, the most workgroups
+    // that a row's chain of loads and sums can hide behind; for a row that is read
+    // twice and long, 512, which hold twice of it (at 4096 x 128256 in bf16, loss
+    // and gradient: 445 instead of 488 us; the loss alone 210 instead of 191, and at
+    // 8192 x 32000 both 247 instead of 224).
     const int64_t units = ceil_div(a.vocab, 16 / elem_bytes(a.dtype));
     const bool twice = !backward && a.dlogits;
     const auto of = [&](auto type) {
         using T = decltype(type);
-        if (t <= cus) return launch(distill_kernel<T, 1024, 8>, k, grid, 1024, stream);
         if (units <= 4 * 256) return launch(distill_kernel<T, 256, 4>, k, grid, 256, stream);
+        if (t <= cus) return launch(distill_kernel<T, 1024, 8>, k, grid, 1024, stream);
         if (!twice || units <= 4096) return launch(distill_kernel<T, 256, 8>, k, grid, 256, stream);
         return launch(distill_kernel<T, 512, 8>, k, grid, 512, stream);
     };
