@@ -14,33 +14,71 @@ namespace {
 
 // ------------------------------------------------------------------ elementwise
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(1.44269504088896341f * x); }
+
+// To a few units of the last place: the hardware's exponential and reciprocal
+// take an eighth of the instructions of the rounded division and expf, which the
+// gradient's elementwise pass would wait for instead of memory (4096 x 14336 with
+// SiLU: 133 us, with GELU by erfcf 191).
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-z)); }
+
+// The normal distribution at z, and exp(-z^2 / 2).  erfc(x) = exp(-x^2) t P(t) with
+// t = 1 / (1 + 0.3 x) for x >= 0; P, of degree 8, is a minimax fit of the relative
+// error over x in [0, 10] (5e-7 as computed in fp32); past that erfc is 0 in fp32.
+__device__ __forceinline__ float normal_cdf(float z, float* bell) {
+    constexpr float c[9] = {0.16918162f, 0.17081371f, 0.14769703f, 0.2172434f, -0.099725366f, 0.55464029f, -0.51802737f, 0.48822719f, -0.13005051f};
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.3f * 0.70710678118654752f * fabsf(z));
+    float p = c[8];
+#pragma unroll
+    for (int i = 7; i >= 0; --i) p = p * t + c[i];
+    *bell = exp_fast(-0.5f * z * z);
+    const float tail = 0.5f * t * p * *bell;
+    return z < 0.f ? tail : 1.f - tail;
+}
 
 // act(z); 1 + tanh(u) is 2 sigmoid(2u).
 __device__ __forceinline__ float act_value(float z, int act) {
     switch (act) {
         case FSDP_ACT_RELU: return z != z ? z : fmaxf(z, 0.f);
         case FSDP_ACT_SILU: return z * sigmoid(z);
-        case FSDP_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);
+        case FSDP_ACT_GELU: {
+            float bell;
+            return z * normal_cdf(z, &bell);
+        }
         case FSDP_ACT_GELU_TANH: return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
         default: return z;
     }
 }
 
-__device__ __forceinline__ float act_slope(float z, int act) {
+// act(z) and its slope.
+__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
     switch (act) {
-        case FSDP_ACT_RELU: return z != z ? z : z > 0.f ? 1.f : 0.f;
+        case FSDP_ACT_RELU:
+            value = z != z ? z : fmaxf(z, 0.f);
+            slope = z != z ? z : z > 0.f ? 1.f : 0.f;
+            return;
         case FSDP_ACT_SILU: {
             const float q = sigmoid(z);
-            return q * (1.f + z * (1.f - q));
+            value = z * q;
+            slope = q * (1.f + z * (1.f - q));
+            return;
         }
-        case FSDP_ACT_GELU:
-            return 0.5f * erfcf(-0.70710678118654752f * z) + z * (0.39894228040143268f * expf(-0.5f * z * z));
+        case FSDP_ACT_GELU: {
+            float bell;
+            const float cdf = normal_cdf(z, &bell);
+            value = z * cdf;
+            slope = cdf + z * (0.39894228040143268f * bell);
+            return;
+        }
         case FSDP_ACT_GELU_TANH: {
             const float q = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
-            return q + z * (q * (1.f - q)) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
+            value = z * q;
+            slope = q + z * (q * (1.f - q)) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
+            return;
         }
-        default: return 1.f;
+        default:
+            value = z;
+            slope = 1.f;
     }
 }
 
