@@ -28,7 +28,7 @@ constexpr int kRowOut = kRows > 2 ? 4 : 2;
 
 template <typename T, int kRows>
 __global__ __launch_bounds__(256) void row_kernel(const Product p) {
-    constexpr int kOut = kRowOut<T, kRows>;
+    constexpr int kOut = kRowOut<T, kRows>, kTogether = 8 / kOut;
     const int lane = threadIdx.x & 63;
     const int64_t j0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * kOut;
     if (j0 >= p.n) return;
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void row_kernel(const Product p) {
         }
     };
     int64_t k = lane * 8;
-#pragma unroll(8 / kOut)
+#pragma unroll kTogether
     for (; k + 8 <= p.k; k += 512) add(k, 8);
     if (k < p.k) add(k, int(p.k - k));
 #pragma unroll

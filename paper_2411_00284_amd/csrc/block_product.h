@@ -104,46 +104,46 @@ struct Product {
     int count;
 };
 
+// What the epilogue reads for eight columns of a row.
+template <typename T>
+struct Extras {
+    Eight<T> times, residual;
+    __device__ __forceinline__ void load(const Epilogue& e, int64_t i, int64_t j, int left) {
+        if (e.times) times = load_some(static_cast<const T*>(e.times) + i * e.times_stride + j, left);
+        if (e.residual) residual = load_some(static_cast<const T*>(e.residual) + i * e.residual_stride + j, left);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ Eight<T> load_bias(const Epilogue& e, int64_t j, int left) {
+    return e.bias && left > 0 ? load_some(static_cast<const T*>(e.bias) + j, left) : Eight<T>(T(0.f));
+}
+
 // z -> out at row i, columns j .. j + 7, of which `left` exist; `z` is the
 // product, without the bias.
 template <typename T>
-__device__ __forceinline__ void finish8(const Epilogue& e, int64_t i, int64_t j, int left, float (&z)[8]) {
-    if (e.bias) {
-        const Eight<T> b = load_some(static_cast<const T*>(e.bias) + j, left);
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t i, int64_t j, int left, const Eight<T>& bias,
+                                        const Extras<T>& x, float (&z)[8]) {
+    if (e.bias)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[c] += float(b[c]);
-    }
+        for (int c = 0; c < 8; ++c) z[c] += float(bias[c]);
     if (e.pre) store_some(static_cast<T*>(e.pre) + i * e.pre_stride + j, left, z);
     if (e.act != FSDP_ACT_NONE)
 #pragma unroll
         for (int c = 0; c < 8; ++c) z[c] = act_value(z[c], e.act);
-    if (e.times) {
-        const Eight<T> f = load_some(static_cast<const T*>(e.times) + i * e.times_stride + j, left);
+    if (e.times)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[c] *= float(f[c]);
-    }
-    if (e.residual) {
-        const Eight<T> r = load_some(static_cast<const T*>(e.residual) + i * e.residual_stride + j, left);
+        for (int c = 0; c < 8; ++c) z[c] *= float(x.times[c]);
+    if (e.residual)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[c] += float(r[c]);
-    }
+        for (int c = 0; c < 8; ++c) z[c] += float(x.residual[c]);
     store_some(static_cast<T*>(e.out) + i * e.out_stride + j, left, z);
 }
-
-// Eight finished or partial sums of row i, columns from j.  kPlain: the product
-// has no epilogue.
-template <typename T, bool kPlain>
-__device__ __forceinline__ void leave8(const Product& p, int part, int64_t i, int64_t j, float (&z)[8]) {
-    if (i >= p.m || j >= p.n) return;
-    const int left = int(min(p.n - j, int64_t(8)));
-    if (p.count > 1) {
-        const int64_t stride = (p.n + 7) / 8 * 8;
-        store_some(p.parts + (part * p.m + i) * stride + j, 8, z);
-    } else if constexpr (kPlain) {
-        store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
-    } else {
-        finish8<T>(p.e, i, j, left, z);
-    }
+template <typename T>
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t i, int64_t j, int left, float (&z)[8]) {
+    Extras<T> x;
+    x.load(e, i, j, left);
+    finish8<T>(e, i, j, left, load_bias<T>(e, j, left), x, z);
 }
 
 // The parts' sums, in order, and the epilogue: a thread takes eight columns.
@@ -439,28 +439,55 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     }
     sync(std::integral_constant<int, 0>());                       // nothing more is written to LDS
 
-    // A wave passes its sums through its own piece of LDS, 32 rows at a time, so
-    // that a lane gets eight neighbouring columns; every other four rows have
-    // their halves of 32 columns exchanged, against conflicts.
-    constexpr int kWide = kTileN / 2, kLanes = kWide / 8;
-    static_assert(B::kBytes == 2 * 32 * kWide * 4 && kWide >= 64, "two waves' pieces");
-    float* const turn = reinterpret_cast<float*>(wave < 2 ? b0 : b1) + wave % 2 * 32 * kWide;
+    // A wave passes its sums through its own piece of LDS, kTurn tiles at a time,
+    // so that a lane gets eight neighbouring columns; every other four rows have
+    // their halves of 32 columns exchanged, against conflicts.  What the epilogue
+    // reads of kAhead rows is asked for before the first of them is finished.
+    constexpr int kWide = kTileN / 2, kLanes = kWide / 8, kTurn = kA > 1 ? 2 : 1, kStepRows = 64 / kLanes, kAhead = 4;
+    static_assert(kWide >= 64 && kTurn * 32 * kWide * 4 <= B::kBytes && kA % kTurn == 0 && kTurn * 32 % (kAhead * kStepRows) == 0 &&
+                  (kSteps == 4 || A::kBytes == B::kBytes));
+    char* const piece = kSteps == 4 ? (wave == 0 ? b0 : wave == 1 ? b1 : wave == 2 ? b2 : b3)
+                                    : (wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? b0 : b1);
+    float* const turn = reinterpret_cast<float*>(piece);
     const auto place = [](int row, int column) { return row * kWide + (column ^ (row / 4 % 2) * 32); };
+    const int column = lane % kLanes * 8;
+    const int64_t j = j0 + wj + column;
+    const int left = int(min(p.n - j, int64_t(8)));
+    const Eight<T> bias = kColumnsB ? Eight<T>(T(0.f)) : load_bias<T>(p.e, j, left);
 #pragma unroll
-    for (int x = 0; x < kA; ++x) {
+    for (int x0 = 0; x0 < kA; x0 += kTurn) {
 #pragma unroll
-        for (int y = 0; y < kB; ++y)
+        for (int x = 0; x < kTurn; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                turn[place(8 * (r / 4) + 4 * (lane / 32) + r % 4, 32 * y + lane % 32)] = acc[x][y][r];
+            for (int y = 0; y < kB; ++y)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    turn[place(32 * x + 8 * (r / 4) + 4 * (lane / 32) + r % 4, 32 * y + lane % 32)] = acc[x0 + x][y][r];
         __builtin_amdgcn_wave_barrier();
+        const int64_t i0x = i0 + wi + 32 * x0;
 #pragma unroll 1
-        for (int r = lane / kLanes; r < 32; r += 64 / kLanes) {
-            const int column = lane % kLanes * 8;
-            float z[8];
+        for (int r0 = lane / kLanes; r0 < 32 * kTurn; r0 += kAhead * kStepRows) {
+            Extras<T> extra[kAhead];
+            if (!kColumnsB && p.count == 1 && left > 0)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) z[c] = turn[place(r, column) + c];
-            leave8<T, kColumnsB>(p, t.part, i0 + wi + 32 * x + r, j0 + wj + column, z);
+                for (int u = 0; u < kAhead; ++u)
+                    if (const int64_t i = i0x + r0 + u * kStepRows; i < p.m) extra[u].load(p.e, i, j, left);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int row = r0 + u * kStepRows;
+                const int64_t i = i0x + row;
+                float z[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) z[c] = turn[place(row, column) + c];
+                if (i >= p.m || left <= 0) continue;
+                if (p.count > 1) {
+                    store_some(p.parts + (t.part * p.m + i) * ((p.n + 7) / 8 * 8) + j, 8, z);
+                } else if constexpr (kColumnsB) {                 // dx and dweight have no epilogue
+                    store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
+                } else {
+                    finish8<T>(p.e, i, j, left, bias, extra[u], z);
+                }
+            }
         }
         __builtin_amdgcn_wave_barrier();
     }
