@@ -3,8 +3,8 @@
 //
 // A product takes one of these forms:
 //   * product_kernel (block_product.h): operands on the 16-byte grid, in tiles of
-//     256 x 256 (16 bits only), 128 x 128 or 64 x 128.  Operands off the grid are
-//     laid on it by a copy into the workspace first.
+//     256 x 256, 64 x 64 (16 bits only), 128 x 128 or 64 x 128.  Operands off the grid
+//     are laid on it by a copy into the workspace first.
 //   * row_kernel: at most four rows of x, at any address.
 // With few tiles the sum over k is cut into parts, which join_parts_kernel joins
 // in order.
@@ -183,6 +183,7 @@ constexpr Form kForms16[] = {
     {128, 128, 2, 2, 0.60, 0.97, 4.0},
     {128, 128, 4, 1, 0.36, 0.52, 3.5},
     {64, 128, 4, 1, 0.25, 0.32, 3.5},
+    {64, 64, 8, 1, 0.14, 0.20, 3.5},
 };
 constexpr Form kForms32[] = {
     {128, 128, 2, 2, 1.80, 3.60, 4.0},
@@ -206,11 +207,17 @@ struct Shape {
 
 constexpr int64_t kMostRows = 4;     // of row_kernel
 
+// Bytes per us in which the operands come out of memory, in all and to one
+// workgroup, and what the caches keep of them: with the second bound, which wants
+// 220 workgroups, 64 x 14336 -> 4096 takes 29.5 us instead of 45, 64 x 28672 -> 8192
+// 104 instead of 140; under 16 MB it would cut products for nothing (64 x 1024 -> 1024
+// 9.1 us instead of 7.2).
+constexpr double kMostRead = 5.5e6, kGroupRead = 0.025e6, kCached = 16e6;
+
 // The form and the cut with the least expected time: whole rounds of workgroups
-// over the CUs, the fullest CU of the last round, reading the operands at 5.5 TB/s
-// if that takes longer, and the join of the parts (3 us, and 8 bytes moved per
-// value and part).  Up to four rows of x, row_kernel reads the weight at HBM's
-// rate in one launch.
+// over the CUs, the fullest CU of the last round, reading the operands if that takes
+// longer, and the join of the parts (3 us, and 8 bytes moved per value and part).
+// Up to four rows of x, row_kernel reads the weight at HBM's rate in one launch.
 Cut choose(const Shape& s, int cus) {
     Cut best;
     if (s.m <= kMostRows && !s.columns_a && !s.columns_b) return best;
@@ -218,10 +225,10 @@ Cut choose(const Shape& s, int cus) {
     const Form* const forms = wide ? kForms32 : kForms16;
     const int step_k = wide ? 32 : 64;
     const int64_t steps = std::max<int64_t>(1, ceil_div(s.k, step_k));
-    const double reading = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k)) / 5.5e6;
+    const double read = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k));
     const double joining = double(s.m) * double(s.n) * 8 / 5e6;
     double least = 0;
-    for (int f = 0; f < (wide ? 2 : 4); ++f) {
+    for (int f = 0; f < (wide ? 2 : 5); ++f) {
         const Form& form = forms[f];
         const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n), slots = int64_t(cus) * form.held;
         for (int parts = 1; parts <= 16; ++parts) {
@@ -232,7 +239,8 @@ Cut choose(const Shape& s, int cus) {
             const int64_t groups = tiles * parts, whole = groups / slots, rest = groups - whole * slots;
             double time = double(whole) * (double(each) * form.full + form.fixed);
             if (rest) time += double(each) * (rest > cus ? form.full : form.alone) + form.fixed;
-            time = std::max(time, reading + form.fixed);
+            const double rate = read > kCached ? std::min(kMostRead, kGroupRead * double(groups)) : kMostRead;
+            time = std::max(time, read / rate + form.fixed);
             if (parts > 1) time += 3.0 + double(parts) * joining;
             if (!best.form || time < least) {
                 least = time;
@@ -288,6 +296,7 @@ fsdp_status launch_tiles(const Product& p, const Cut& c, fsdp_dtype dtype, hipSt
     const auto of = [&](auto type) {
         using T = decltype(type);
         if (f.tile_m == 256) return launch(product_kernel<T, kColumnsA, kColumnsB, 256, 256, 2>, p, grid, 256, stream);
+        if (f.tile_n == 64) return launch(product_kernel<T, kColumnsA, kColumnsB, 64, 64, 8>, p, grid, 256, stream);
         if (f.tile_m == 64) return launch(product_kernel<T, kColumnsA, kColumnsB, 64, 128, 4>, p, grid, 256, stream);
         return f.steps == 2 ? launch(product_kernel<T, kColumnsA, kColumnsB, 128, 128, 2>, p, grid, 256, stream)
                             : launch(product_kernel<T, kColumnsA, kColumnsB, 128, 128, 4>, p, grid, 256, stream);

@@ -339,9 +339,11 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     constexpr int kDeep = A::kDeep;
     constexpr int kA = kTileM / 64, kB = kTileN / 64;            // 32-row tiles of a wave
     // One array per step: their reads and loads are known not to touch each other.
-    __shared__ __attribute__((aligned(1024))) char a0[A::kBytes], a1[A::kBytes], a2[kSteps > 2 ? A::kBytes : 16],
-        a3[kSteps > 2 ? A::kBytes : 16], b0[B::kBytes], b1[B::kBytes], b2[kSteps > 2 ? B::kBytes : 16], b3[kSteps > 2 ? B::kBytes : 16];
-    static_assert(kSteps == 2 || kSteps == 4);
+    constexpr int kA4 = kSteps > 2 ? A::kBytes : 16, kB4 = kSteps > 2 ? B::kBytes : 16;
+    constexpr int kA8 = kSteps > 4 ? A::kBytes : 16, kB8 = kSteps > 4 ? B::kBytes : 16;
+    __shared__ __attribute__((aligned(1024))) char a0[A::kBytes], a1[A::kBytes], a2[kA4], a3[kA4], a4[kA8], a5[kA8], a6[kA8], a7[kA8];
+    __shared__ __attribute__((aligned(1024))) char b0[B::kBytes], b1[B::kBytes], b2[kB4], b3[kB4], b4[kB8], b5[kB8], b6[kB8], b7[kB8];
+    static_assert(kSteps == 2 || kSteps == 4 || kSteps == 8);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wi = wave / 2 * (kTileM / 2), wj = wave % 2 * (kTileN / 2);
     const TilePlace t = tile_place(blockIdx.x, unsigned((p.m + kTileM - 1) / kTileM), unsigned((p.n + kTileN - 1) / kTileN),
@@ -423,6 +425,12 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
         ask(a2, b2);
         ask(a3, b3);
     }
+    if constexpr (kSteps > 4) {
+        ask(a4, b4);
+        ask(a5, b5);
+        ask(a6, b6);
+        ask(a7, b7);
+    }
     sync(std::integral_constant<int, kSteps - 1>());
     fa[0].read(a0, pa, 0);
     fb[0].read(b0, pb, 0);
@@ -434,7 +442,15 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
         } else {
             step(a1, b1, a2, b2);
             step(a2, b2, a3, b3);
-            step(a3, b3, a0, b0);
+            if constexpr (kSteps == 4) {
+                step(a3, b3, a0, b0);
+            } else {
+                step(a3, b3, a4, b4);
+                step(a4, b4, a5, b5);
+                step(a5, b5, a6, b6);
+                step(a6, b6, a7, b7);
+                step(a7, b7, a0, b0);
+            }
         }
     }
     sync(std::integral_constant<int, 0>());                       // nothing more is written to LDS
@@ -443,13 +459,14 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     // so that a lane gets eight neighbouring columns; every other four rows have
     // their halves of 32 columns exchanged, against conflicts.  What the epilogue
     // reads of kAhead rows is asked for before the first of them is finished.
-    constexpr int kWide = kTileN / 2, kLanes = kWide / 8, kTurn = kA > 1 ? 2 : 1, kStepRows = 64 / kLanes, kAhead = 4;
-    static_assert(kWide >= 64 && kTurn * 32 * kWide * 4 <= B::kBytes && kA % kTurn == 0 && kTurn * 32 % (kAhead * kStepRows) == 0 &&
-                  (kSteps == 4 || A::kBytes == B::kBytes));
-    char* const piece = kSteps == 4 ? (wave == 0 ? b0 : wave == 1 ? b1 : wave == 2 ? b2 : b3)
+    constexpr int kWide = kTileN / 2, kLanes = kWide / 8, kTurn = kA > 1 ? 2 : 1, kStepRows = 64 / kLanes,
+                  kAhead = kTurn * 32 / kStepRows < 4 ? kTurn * 32 / kStepRows : 4;
+    static_assert(kTurn * 32 * kWide * 4 <= B::kBytes && kA % kTurn == 0 && kTurn * 32 % (kAhead * kStepRows) == 0 &&
+                  (kSteps > 2 || A::kBytes == B::kBytes));
+    char* const piece = kSteps > 2 ? (wave == 0 ? b0 : wave == 1 ? b1 : wave == 2 ? b2 : b3)
                                     : (wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? b0 : b1);
     float* const turn = reinterpret_cast<float*>(piece);
-    const auto place = [](int row, int column) { return row * kWide + (column ^ (row / 4 % 2) * 32); };
+    const auto place = [](int row, int column) { return row * kWide + (column ^ (kWide > 32 ? row / 4 % 2 * 32 : 0)); };
     const int column = lane % kLanes * 8;
     const int64_t j = j0 + wj + column;
     const int left = int(min(p.n - j, int64_t(8)));

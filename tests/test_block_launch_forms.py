@@ -143,11 +143,11 @@ def test_every_kernel_is_reached(launches):
     for d in (BF16, F16, F32):
         calls += [linear(m, 4096, 4096, d) for m in (1, 2, 4)]
         calls += [linear(m, n, k, d) for m, n, k in ((16, 4096, 4096), (1024, 4096, 4096), (2048, 4096, 4096), (8192, 8192, 8192),
-                                                     (300, 257, 8191), (64, 256, 8192))]
+                                                     (300, 257, 8191), (64, 256, 8192), (128, 14336, 1024))]
         calls += [linear_grad(m, n, k, d, 2, dx=at(5), dweight=at(6), dbias=at(7))
                   for m, n, k in ((64, 4096, 64), (64, 256, 8192), (1024, 4096, 4096), (2048, 4096, 4096), (4096, 1024, 4096),
                                   (512, 2048, 512), (8192, 8192, 8192), (4096, 2048, 2048), (1024, 2048, 4096), (256, 512, 1024), (4096, 4096, 1024),
-                                  (8192, 4096, 14336))]
+                                  (8192, 4096, 14336), (128, 1024, 14336), (1024, 128, 14336))]
         for tokens, vocab in ((5, 32000), (5000, 1000), (5000, 6000), (5000, 128256)):
             calls += [distill(tokens, vocab, d), distill(tokens, vocab, d, grad=True)]
     _, mangled, built = launches(calls)

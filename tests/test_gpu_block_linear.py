@@ -77,6 +77,14 @@ FORWARD = [
     (300, 260, 700, "f32", None, False, False, True, False, 4, 4),
     (1000, 688, 256, "f32", "gelu", True, True, True, True, 0, 0),
     (2049, 4104, 72, "bf16", "silu", False, True, False, False, 0, 0),
+    # The other tiles, and tiles whose sum over k is cut.
+    (776, 1287, 72, "bf16", "silu", True, True, True, True, 1, 0),
+    (136, 2056, 4104, "f16", "gelu", True, False, True, False, 8, 0),
+    (8200, 136, 72, "bf16", "gelu_tanh", True, True, False, True, 0, 0),
+    (2056, 136, 8200, "f16", None, True, False, True, False, 0, 8),
+    (391, 8200, 72, "f16", "relu", False, True, True, True, 8, 0),
+    (520, 14344, 72, "bf16", None, True, False, False, False, 0, 0),
+    (8200, 136, 8200, "bf16", "silu", False, False, True, True, 0, 0),
 ]
 
 
@@ -215,6 +223,15 @@ GRADIENT = [
     (2048, 136, 2048, "f16", None, False, False, 0, 0),
     (4100, 72, 96, "bf16", "silu", False, True, 0, 0),
     (1000, 688, 256, "f32", "gelu", False, True, 4, 4),
+    # The other tiles, for dx and for dweight.
+    (776, 72, 1287, "bf16", "silu", True, True, 1, 0),
+    (8200, 72, 136, "f16", None, False, True, 0, 0),
+    (391, 72, 8200, "bf16", "gelu", False, False, 8, 0),
+    (520, 72, 14344, "f16", "relu", True, True, 0, 0),
+    (72, 776, 1288, "f16", "gelu", False, True, 0, 8),
+    (72, 8200, 136, "bf16", None, True, False, 0, 0),
+    (72, 391, 8200, "f16", "silu", False, True, 0, 0),
+    (72, 520, 14344, "bf16", None, False, True, 0, 0),
 ]
 
 
