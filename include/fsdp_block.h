@@ -158,8 +158,8 @@ typedef struct fsdp_linear_args {
 
 fsdp_status fsdp_block_linear_workspace(const fsdp_linear_args* args, int64_t* bytes);
 /* One kernel; one before it where x or weight lies off the 16-byte grid (up to
- * four rows of x excepted), one after it where few tiles split the sum over k.
- * None where out has no elements. */
+ * four rows of x excepted), one after it where few tiles split the sum over k,
+ * or many leave a last round of few.  None where out has no elements. */
 fsdp_status fsdp_block_linear(const fsdp_linear_args* args, void* workspace, int64_t workspace_bytes,
                               hipStream_t stream);
 
@@ -194,8 +194,7 @@ typedef struct fsdp_linear_grad_args {
 
 fsdp_status fsdp_block_linear_grad_workspace(const fsdp_linear_grad_args* args, int64_t* bytes);
 /* At most one kernel for dz and its sums, one to join the sums, and for each
- * product one; one more before it where a factor lies off the 16-byte grid,
- * and one after it where it is split. */
+ * product as many as fsdp_block_linear. */
 fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args, void* workspace, int64_t workspace_bytes,
                                    hipStream_t stream);
 

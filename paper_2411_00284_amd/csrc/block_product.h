@@ -102,6 +102,7 @@ struct Product {
     float* parts;
     int64_t part_k;
     int count;
+    int64_t first_i, first_j;        // the tiles begin there and go to m and n
 };
 
 // What the epilogue reads for eight columns of a row.
@@ -352,9 +353,9 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     static_assert(kSteps == 2 || kSteps == 4 || kSteps == 8);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wi = wave / 2 * (kTileM / 2), wj = wave % 2 * (kTileN / 2);
-    const TilePlace t = tile_place(blockIdx.x, unsigned((p.m + kTileM - 1) / kTileM), unsigned((p.n + kTileN - 1) / kTileN),
+    const TilePlace t = tile_place(blockIdx.x, unsigned((p.m - p.first_i + kTileM - 1) / kTileM), unsigned((p.n - p.first_j + kTileN - 1) / kTileN),
                                    unsigned(p.count));
-    const int64_t i0 = int64_t(t.row) * kTileM, j0 = int64_t(t.column) * kTileN;
+    const int64_t i0 = p.first_i + int64_t(t.row) * kTileM, j0 = p.first_j + int64_t(t.column) * kTileN;
     const int64_t k0 = t.part * p.part_k, k1 = min(k0 + p.part_k, p.k);
     A a(p.a, p.a_stride, i0, p.m, k0, k1);
     B b(p.b, p.b_stride, j0, p.n, k0, k1);

@@ -121,6 +121,9 @@ def test_launches_per_call(launches):
         linear(64, 256, 8192),
         linear(700, 700, 701),
         linear(0, 4096, 4096),
+        linear(4096, 14336, 4096),
+        linear(4101, 4104, 520),
+        linear(1020, 18440, 520),
         linear_grad(4096, 4096, 4096, dx=at(5), dweight=at(6)),
         linear_grad(4096, 4096, 4096, act=2, dx=at(5), dweight=at(6), dbias=at(7)),
         linear_grad(0, 64, 64, dx=at(5), dweight=at(6), dbias=at(7)),
@@ -129,7 +132,7 @@ def test_launches_per_call(launches):
         distill(100, 32000, BF16, grad=True, backward=True),
         distill(0, 32000, BF16),
     ])
-    assert [len(n) for n in names] == [1, 2, 1, 1, 1, 1, 1, 2, 2, 0, 2, 4, 2, 1, 1, 1, 0]
+    assert [len(n) for n in names] == [1, 2, 1, 1, 1, 1, 1, 2, 2, 0, 2, 2, 2, 2, 4, 2, 1, 1, 1, 0]
     assert "row_kernel" in names[5][0] and "join_parts" in names[7][1] and "pad_kernel" in names[8][0]
 
 

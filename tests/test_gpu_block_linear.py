@@ -85,6 +85,9 @@ FORWARD = [
     (391, 8200, 72, "f16", "relu", False, True, True, True, 8, 0),
     (520, 14344, 72, "bf16", None, True, False, False, False, 0, 0),
     (8200, 136, 8200, "bf16", "silu", False, False, True, True, 0, 0),
+    # A last round of tiles of its own: rows, columns.
+    (4101, 4104, 520, "bf16", "silu", True, True, False, True, 8, 0),
+    (1020, 18437, 520, "f16", None, True, False, True, False, 3, 0),
 ]
 
 
@@ -232,6 +235,9 @@ GRADIENT = [
     (72, 8200, 136, "bf16", None, True, False, 0, 0),
     (72, 391, 8200, "f16", "silu", False, True, 0, 0),
     (72, 520, 14344, "bf16", None, False, True, 0, 0),
+    # A last round of tiles of its own, for dx and for dweight.
+    (4101, 520, 4104, "bf16", None, False, False, 8, 0),
+    (520, 1020, 18437, "f16", "relu", False, True, 0, 0),
 ]
 
 
