@@ -466,6 +466,9 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     // so that a lane gets eight neighbouring columns; every other four rows have
     // their halves of 32 columns exchanged, against conflicts.  What the epilogue
     // reads of kAhead rows is asked for before the first of them is finished.
+    // No other wave touches the piece, so no barrier of the workgroup is needed; the fences
+    // keep the lanes' writes before the reads of other lanes', and those before the next
+    // writes.
     constexpr int kWide = kTileN / 2, kLanes = kWide / 8, kTurn = kA > 1 ? 2 : 1, kStepRows = 64 / kLanes,
                   kAhead = kTurn * 32 / kStepRows < 4 ? kTurn * 32 / kStepRows : 4;
     static_assert(kTurn * 32 * kWide * 4 <= B::kBytes && kA % kTurn == 0 && kTurn * 32 % (kAhead * kStepRows) == 0 &&
@@ -487,6 +490,7 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     turn[place(32 * x + 8 * (r / 4) + 4 * (lane / 32) + r % 4, 32 * y + lane % 32)] = acc[x0 + x][y][r];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         const int64_t i0x = i0 + wi + 32 * x0;
 #pragma unroll 1
@@ -513,6 +517,7 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
                 }
             }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
 }
