@@ -20,7 +20,9 @@
  *   - A pointer may be NULL where a comment says "or NULL", or where the
  *     matrix has no elements.
  *   - Outputs must not overlap inputs or each other, except that an output may
- *     BE an input (same pointer, stride and type) where a comment says so.
+ *     BE an input (same pointer, stride and type) where a comment says so.  An
+ *     input that other rows or columns read too (a weight, a bias, a gate, the
+ *     factors of a product) may not lie there even then.
  *     Matrices of one row stride may interleave (column slices of one buffer).
  *   - Sums, statistics and products are held in fp32; each output is rounded
  *     once, to nearest even, unless a comment says otherwise.  Results do not

@@ -331,8 +331,8 @@ fsdp_status run(const fsdp_distill_args* args, bool backward, hipStream_t stream
     if (!backward && a.tokens > 0 && !a.loss && !a.lse && !a.dlogits) return fail(FSDP_ERR_INVALID, "no output is wanted");
     const int64_t t = a.tokens;
     Checked m;
-    m.add("logits", a.logits, t, a.vocab, a.logits_stride, a.dtype, true);
-    m.add("teacher", a.teacher, t, a.top, a.top, a.teacher_dtype, true);
+    m.add_in_place("logits", a.logits, t, a.vocab, a.logits_stride, a.dtype, true);
+    m.add_in_place("teacher", a.teacher, t, a.top, a.top, a.teacher_dtype, true);
     // int64 ids: twice as many fp32-sized elements
     m.add("ids", a.ids, t, a.top << a.ids_64, a.top << a.ids_64, FSDP_DTYPE_F32, true);
     if (a.ids && a.ids_64 && reinterpret_cast<uintptr_t>(a.ids) % 8 != 0) return fail(FSDP_ERR_ALIGN, "ids is not element-aligned");

@@ -83,7 +83,7 @@ void Checked::add(const char* name, const void* p, int64_t rows, int64_t cols, i
         st_ = fail(FSDP_ERR_TOO_MANY, "too many arguments to check");
         return;
     }
-    m_[n_++] = {name, p, rows, cols, stride, esize, output, {alias0, alias1}};
+    m_[n_++] = {name, p, rows, cols, stride, dtype, esize, output, false, {alias0, alias1}};
 }
 
 fsdp_status Checked::done() {
@@ -91,8 +91,8 @@ fsdp_status Checked::done() {
         if (!m_[i].output) continue;
         for (int j = 0; j < n_; ++j) {
             if (j == i || (m_[j].output && j < i) || !overlap(m_[i], m_[j])) continue;
-            const bool same = m_[i].p == m_[j].p && m_[i].stride == m_[j].stride && m_[i].esize == m_[j].esize;
-            if (!m_[j].output && same && (m_[i].alias[0] == m_[j].p || m_[i].alias[1] == m_[j].p)) continue;
+            const bool same = m_[i].p == m_[j].p && m_[i].stride == m_[j].stride && m_[i].dtype == m_[j].dtype;
+            if (m_[j].in_place && same && (m_[i].alias[0] == m_[j].p || m_[i].alias[1] == m_[j].p)) continue;
             st_ = fail(FSDP_ERR_OVERLAP, "%s overlaps %s", m_[i].name, m_[j].name);
             break;
         }

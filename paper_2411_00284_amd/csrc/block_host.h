@@ -26,8 +26,10 @@ struct Matrix {
     const char* name;
     const void* p;
     int64_t rows, cols, stride;      // stride in elements; rows of `cols` contiguous elements
+    fsdp_dtype dtype;
     int esize;
     bool output;
+    bool in_place;                   // an input that a kernel reads where it writes, and nowhere else
     const void* alias[2];            // inputs that this output may be
     int64_t lo() const { return int64_t(reinterpret_cast<uintptr_t>(p)); }
     bool empty() const { return rows == 0 || cols == 0; }
@@ -39,9 +41,17 @@ struct Matrix {
 class Checked {
 public:
     // `needed`: may not be NULL unless it is empty.  A NULL matrix is left out.
-    // An output takes the inputs it may be, which must have its type.
+    // An output takes the inputs it may be, which must have its stride and type.
     void add(const char* name, const void* p, int64_t rows, int64_t cols, int64_t stride, fsdp_dtype dtype, bool needed,
              bool output = false, const void* alias0 = nullptr, const void* alias1 = nullptr);
+    // An input that an output may be: every value is read before it is written, by the
+    // thread or workgroup that writes it.  Others may not lie there, whatever their address
+    // (a gate's row that is the first row of the stream, x that is the residual too).
+    void add_in_place(const char* name, const void* p, int64_t rows, int64_t cols, int64_t stride, fsdp_dtype dtype, bool needed) {
+        const int before = n_;
+        add(name, p, rows, cols, stride, dtype, needed);
+        if (n_ > before) m_[before].in_place = true;
+    }
     void add_vector(const char* name, const void* p, int64_t n, fsdp_dtype dtype, bool needed, bool output = false) {
         add(name, p, n > 0 ? 1 : 0, n, n, dtype, needed, output);
     }

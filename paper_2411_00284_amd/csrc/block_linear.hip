@@ -419,8 +419,8 @@ fsdp_status check_linear(const fsdp_linear_args& a) {
     c.add("x", a.x, a.m, a.k, a.x_stride, a.dtype, a.n > 0);
     c.add("weight", a.weight, a.n, a.k, a.weight_stride, a.dtype, a.m > 0);
     c.add_vector("bias", a.bias, a.n, a.dtype, false);
-    c.add("times", a.times, a.m, a.n, a.times_stride, a.dtype, false);
-    c.add("residual", a.residual, a.m, a.n, a.residual_stride, a.dtype, false);
+    c.add_in_place("times", a.times, a.m, a.n, a.times_stride, a.dtype, false);
+    c.add_in_place("residual", a.residual, a.m, a.n, a.residual_stride, a.dtype, false);
     c.add("pre", a.pre, a.m, a.n, a.pre_stride, a.dtype, false, true);
     c.add("out", a.out, a.m, a.n, a.out_stride, a.dtype, true, true, a.times, a.residual);
     return c.done();
@@ -433,11 +433,11 @@ fsdp_status check_grad(const fsdp_linear_grad_args& a) {
     const bool slopes = a.dx || a.dweight || a.dbias;
     if (a.dtimes && !a.times && a.m > 0) return fail(FSDP_ERR_INVALID, "dtimes needs times");
     Checked c;
-    c.add("dout", a.dout, a.m, a.n, a.dout_stride, a.dtype, any);
+    c.add_in_place("dout", a.dout, a.m, a.n, a.dout_stride, a.dtype, any);
     c.add("x", a.x, a.m, a.k, a.x_stride, a.dtype, a.dweight && a.n > 0);
     c.add("weight", a.weight, a.n, a.k, a.weight_stride, a.dtype, a.dx && a.m > 0);
-    c.add("pre", a.pre, a.m, a.n, a.pre_stride, a.dtype, a.dtimes || (slopes && a.activation != FSDP_ACT_NONE));
-    c.add("times", a.times, a.m, a.n, a.times_stride, a.dtype, false);
+    c.add_in_place("pre", a.pre, a.m, a.n, a.pre_stride, a.dtype, a.dtimes || (slopes && a.activation != FSDP_ACT_NONE));
+    c.add_in_place("times", a.times, a.m, a.n, a.times_stride, a.dtype, false);
     c.add("dx", a.dx, a.m, a.k, a.dx_stride, a.dtype, false, true);
     c.add("dweight", a.dweight, a.n, a.k, a.dweight_stride, a.dtype, false, true);
     c.add_vector("dbias", a.dbias, a.n, a.dtype, false, true);

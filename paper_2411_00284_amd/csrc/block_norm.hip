@@ -457,10 +457,10 @@ fsdp_status check_grad(const fsdp_norm_grad_args& a) {
     if (a.tokens == 0 && a.gate_rows > 60000) return fail(FSDP_ERR_OVERFLOW, "too many rows of the gate without tokens");
     Checked m;
     const int64_t t = a.tokens, h = a.hidden;
-    m.add("y", a.y, t, h, a.y_stride, a.stream_dtype, a.dh);
-    m.add("dy", a.dy, t, h, a.dy_stride, a.stream_dtype, false);
-    m.add("dh", a.dh, t, h, a.dh_stride, a.block_dtype, false);
-    m.add("branch", a.branch, t, h, a.branch_stride, a.block_dtype, false);
+    m.add_in_place("y", a.y, t, h, a.y_stride, a.stream_dtype, a.dh);
+    m.add_in_place("dy", a.dy, t, h, a.dy_stride, a.stream_dtype, false);
+    m.add_in_place("dh", a.dh, t, h, a.dh_stride, a.block_dtype, false);
+    m.add_in_place("branch", a.branch, t, h, a.branch_stride, a.block_dtype, false);
     m.add_vector("post_weight", a.post_weight, h, a.weight_dtype, false);
     m.add("gate", a.gate, a.gate_rows, h, h, a.block_dtype, false);
     m.add_vector("pre_weight", a.pre_weight, h, a.weight_dtype, false);
@@ -487,8 +487,8 @@ extern "C" fsdp_status fsdp_block_norm(const fsdp_norm_args* args, hipStream_t s
     if (a.tokens > 0 && !a.y && !a.h) return fail(FSDP_ERR_INVALID, "neither y nor h is wanted");
     if (a.tokens > 0 && a.h && !a.pre_weight) return fail(FSDP_ERR_INVALID, "h needs pre_weight");
     Checked m;
-    m.add("x", a.x, a.tokens, a.hidden, a.x_stride, a.stream_dtype, true);
-    m.add("branch", a.branch, a.tokens, a.hidden, a.branch_stride, a.block_dtype, false);
+    m.add_in_place("x", a.x, a.tokens, a.hidden, a.x_stride, a.stream_dtype, true);
+    m.add_in_place("branch", a.branch, a.tokens, a.hidden, a.branch_stride, a.block_dtype, false);
     m.add_vector("post_weight", a.post_weight, a.hidden, a.weight_dtype, false);
     m.add("gate", a.gate, a.gate_rows, a.hidden, a.hidden, a.block_dtype, false);
     m.add_vector("pre_weight", a.pre_weight, a.hidden, a.weight_dtype, false);
