@@ -134,6 +134,12 @@ fsdp_status fsdp_block_norm_grad(const fsdp_norm_grad_args* args, void* workspac
  * x [m, k], weight [n, k] (a parameter as the copy-out leaves it), bias [n],
  * times, residual, pre and out [m, n], all of one type.  `pre` keeps z,
  * rounded, for the gradient; out is computed from z before that.
+ *
+ * Sizes are at most 2^30, with 2^22 tiles of 64 x 64 in every matrix.  With more than
+ * four rows of x, 64 rows of x and of weight (fp32: 64 and 128; all, if there are fewer)
+ * must lie within 2^31 bytes, at rows of k in whole 128-byte lines: k up to 17 million in
+ * 16 bits, 4.2 million in fp32.  The gradient's products ask the same of n for dz, and of k
+ * and n 17 million.  Else FSDP_ERR_OVERFLOW.
  */
 typedef int32_t fsdp_activation;
 enum {

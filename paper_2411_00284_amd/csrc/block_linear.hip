@@ -207,9 +207,25 @@ struct Shape {
     int64_t m, n, k;
     fsdp_dtype dtype;
     bool columns_a, columns_b;
+    int64_t stride_a, stride_b;      // of the operands as they are laid on the grid
 };
 
+// The most bytes that a load may lie from its tile's first (Operand::load), and
+// whether a form's loads stay within: an operand by rows has the tile's rows in a
+// step, one by columns the step's rows of k (all of them: past the last it reads
+// the zeros after the operand).  Without k nothing is loaded.
+constexpr int64_t kReach = 0x7ffffff0;
+bool reaches(const Form& f, const Shape& s) {
+    if (s.k == 0) return true;
+    const int64_t size = elem_bytes(s.dtype), deep = 128 / size;
+    const auto end = [&](bool columns, int64_t rows, int64_t tile, int64_t stride) {
+        return columns ? ((deep - 1) * stride + tile) * size : (std::min(tile, rows) - 1) * stride * size + 128;
+    };
+    return end(s.columns_a, s.m, f.tile_m, s.stride_a) <= kReach && end(s.columns_b, s.n, f.tile_n, s.stride_b) <= kReach;
+}
+
 constexpr int64_t kMostRows = 4;     // of row_kernel
+bool row_form(const Shape& s) { return s.m <= kMostRows && !s.columns_a && !s.columns_b; }
 
 // Bytes per us in which the operands come out of memory, in all and to one
 // workgroup, and what the caches keep of them: with the second bound, which wants
@@ -235,7 +251,7 @@ double rounds_time(const Form& form, int64_t groups, int64_t steps, int cus) {
 // instead of 791.  (Smaller tiles for the rest: 334 instead of 300 us at 5000^3.)
 Cut choose(const Shape& s, int cus) {
     Cut best;
-    if (s.m <= kMostRows && !s.columns_a && !s.columns_b) return best;
+    if (row_form(s)) return best;
     const bool wide = s.dtype == FSDP_DTYPE_F32;
     const Form* const forms = wide ? kForms32 : kForms16;
     const int step_k = wide ? 32 : 64;
@@ -245,6 +261,7 @@ Cut choose(const Shape& s, int cus) {
     double least = 0;
     for (int f = 0; f < (wide ? 2 : 5); ++f) {
         const Form& form = forms[f];
+        if (!reaches(form, s)) continue;
         const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n);
         for (int parts = 1; parts <= 16; ++parts) {
             // Parts of at least four steps, and no more of them than some rounds.
@@ -266,6 +283,7 @@ Cut choose(const Shape& s, int cus) {
     }
     if (wide || s.m == 0 || s.n == 0) return best;
     const Form &big = forms[0], &small = forms[1];
+    if (!reaches(big, s)) return best;
     const int64_t down = ceil_div(s.m, big.tile_m), across = ceil_div(s.n, big.tile_n);
     for (const bool rows : {true, false}) {
         // Rows (columns) of tiles in whole rounds, and what is left of out.
@@ -300,6 +318,17 @@ int64_t lined(int64_t cols, fsdp_dtype dtype) { return round_up(cols, 128 / elem
 bool on_grid(const Source& o, fsdp_dtype dtype) {
     const int unit = 16 / elem_bytes(dtype);
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % unit == 0 && o.stride < (1 << 21) && (o.zeros || o.cols % unit == 0);
+}
+
+// A row's stride where product_kernel reads it.
+int64_t laid_stride(const Source& o, fsdp_dtype dtype) { return on_grid(o, dtype) ? o.stride : lined(o.cols, dtype); }
+
+// Whether any form reaches the operands (row_kernel reaches all of its).
+fsdp_status check_reach(const Shape& s) {
+    if (s.m == 0 || s.n == 0 || row_form(s)) return FSDP_OK;
+    if (s.dtype == FSDP_DTYPE_F32 ? reaches(kForms32[1], s) : reaches(kForms16[4], s)) return FSDP_OK;
+    return fail(FSDP_ERR_OVERFLOW, "a tile's rows of an operand of %lld x %lld, %lld x %lld do not lie within 2^31 bytes",
+                (long long)s.m, (long long)s.k, (long long)s.n, (long long)s.k);
 }
 
 // Adds a product's needs to those of `bytes`.
@@ -448,13 +477,26 @@ fsdp_status check_grad(const fsdp_linear_grad_args& a) {
 int64_t row_stride(int64_t rows, int64_t cols, int64_t stride) { return rows > 1 ? stride : round_up(cols, 8); }
 
 // The operands of the three products.
-Shape forward_shape(const fsdp_linear_args& a) { return {a.m, a.n, a.k, a.dtype, false, false}; }
 Source forward_x(const fsdp_linear_args& a) { return {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false}; }
 Source forward_w(const fsdp_linear_args& a) { return {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false}; }
+Shape forward_shape(const fsdp_linear_args& a) {
+    return {a.m, a.n, a.k, a.dtype, false, false, laid_stride(forward_x(a), a.dtype), laid_stride(forward_w(a), a.dtype)};
+}
+
+bool dz_is_dout(const fsdp_linear_grad_args& a) { return !a.times && a.activation == FSDP_ACT_NONE; }
+Source grad_dz(const fsdp_linear_grad_args& a, bool kept, const void* at) {
+    if (kept) return {at, a.m, a.n, lined(a.n, a.dtype), true};
+    return {a.dout, a.m, a.n, row_stride(a.m, a.n, a.dout_stride), false};
+}
+// dx = dz weight, or dweight = dz^T x: `other` is weight or x.
+Shape grad_shape(const fsdp_linear_grad_args& a, bool dweight, const Source& dz, const Source& other) {
+    const int64_t first = laid_stride(dz, a.dtype), second = laid_stride(other, a.dtype);
+    return dweight ? Shape{a.n, a.k, a.m, a.dtype, true, true, first, second}
+                   : Shape{a.m, a.k, a.n, a.dtype, false, true, first, second};
+}
 
 // What a gradient needs besides its outputs.
 struct GradParts {
-    bool slopes = false;             // dz is not dout
     int64_t parts = 0, part_rows = 1;            // row parts of dbias
     int64_t dz = -1, dbias = -1;     // byte offsets
     int64_t bytes = 0;               // of the workspace
@@ -463,14 +505,22 @@ struct GradParts {
     Cut dx, dw;
 };
 
+fsdp_status check_reach(const fsdp_linear_grad_args& a) {
+    const Source dz = grad_dz(a, !dz_is_dout(a), nullptr);
+    if (a.dx) {
+        const fsdp_status st = check_reach(grad_shape(a, false, dz, {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false}));
+        if (st != FSDP_OK) return st;
+    }
+    return a.dweight ? check_reach(grad_shape(a, true, dz, {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false})) : FSDP_OK;
+}
+
 GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
     GradParts g;
-    g.slopes = a.times || a.activation != FSDP_ACT_NONE;
     if (a.m > 0 && a.n > 0) {
         const int64_t columns = ceil_div(a.n, 512);
         g.part_rows = std::max<int64_t>(4, round_up(ceil_div(a.m * columns, 8 * int64_t(cus)), 4));
         g.parts = ceil_div(a.m, g.part_rows);
-        if (g.slopes && (a.dx || a.dweight)) {
+        if (!dz_is_dout(a) && (a.dx || a.dweight)) {
             g.dz = g.bytes;
             g.bytes += round_up(a.m * lined(a.n, a.dtype) * elem_bytes(a.dtype), 256);
         }
@@ -479,13 +529,11 @@ GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
             g.bytes += round_up(g.parts * a.n * 4, 256);
         }
     }
-    const void* const dz = g.dz >= 0 ? ws + g.dz : a.dout;
-    const int64_t stride = g.dz >= 0 ? lined(a.n, a.dtype) : row_stride(a.m, a.n, a.dout_stride);
-    g.from_dz = {dz, a.m, a.n, stride, g.dz >= 0};
+    g.from_dz = grad_dz(a, g.dz >= 0, ws + std::max<int64_t>(g.dz, 0));
     g.weight = {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false};
     g.x = {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false};
-    g.dx_shape = {a.m, a.k, a.n, a.dtype, false, true};
-    g.dw_shape = {a.n, a.k, a.m, a.dtype, true, true};
+    g.dx_shape = grad_shape(a, false, g.from_dz, g.weight);
+    g.dw_shape = grad_shape(a, true, g.from_dz, g.x);
     const int64_t own = g.bytes;
     // The two products follow each other on the stream: they share what they need.
     if (a.dx) {
@@ -508,6 +556,7 @@ extern "C" fsdp_status fsdp_block_linear_workspace(const fsdp_linear_args* args,
     clear_error();
     if (!args || !bytes) return fail(FSDP_ERR_INVALID, "args or bytes is NULL");
     fsdp_status st = check_linear(*args);
+    if (st == FSDP_OK) st = check_reach(forward_shape(*args));
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
@@ -521,6 +570,7 @@ extern "C" fsdp_status fsdp_block_linear(const fsdp_linear_args* args, void* wor
     if (!args) return fail(FSDP_ERR_INVALID, "args is NULL");
     const fsdp_linear_args& a = *args;
     fsdp_status st = check_linear(a);
+    if (st == FSDP_OK) st = check_reach(forward_shape(a));
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
@@ -537,6 +587,7 @@ extern "C" fsdp_status fsdp_block_linear_grad_workspace(const fsdp_linear_grad_a
     clear_error();
     if (!args || !bytes) return fail(FSDP_ERR_INVALID, "args or bytes is NULL");
     fsdp_status st = check_grad(*args);
+    if (st == FSDP_OK) st = check_reach(*args);
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
@@ -550,6 +601,7 @@ extern "C" fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args,
     if (!args) return fail(FSDP_ERR_INVALID, "args is NULL");
     const fsdp_linear_grad_args& a = *args;
     fsdp_status st = check_grad(a);
+    if (st == FSDP_OK) st = check_reach(a);
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;

@@ -270,7 +270,8 @@ struct Operand {
         }
     }
 
-    // Asks for the next step, with `rest` k left, into `lds`.
+    // Asks for the next step, with `rest` k left, into `lds`.  Offsets are 32 bits from
+    // the tile's first byte, and none passes kMost: the host takes no form of larger ones.
     __device__ __forceinline__ void load(char* lds, int64_t rest) {
         typedef __attribute__((address_space(3))) void lds_void;
         constexpr uint32_t kMost = 0x7ffffff0u, kNowhere = 0xfffffff0u;
