@@ -5,6 +5,8 @@
 #include "block_device.h"
 #include "block_host.h"
 
+#include <algorithm>
+
 namespace fsdp_block {
 namespace {
 
@@ -20,6 +22,7 @@ struct JoinArgs {
 // A line of 32 columns per workgroup and 32 rows of parts at a time: many
 // workgroups, each with few loads to wait for one after the other.
 constexpr int kJoinColumns = 32, kJoinThreads = 1024;
+constexpr int64_t kJoinGrid = int64_t(1) << 21;      // workgroups along the columns: below 2^32 threads
 
 template <typename TB>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const JoinArgs a) {
@@ -27,21 +30,25 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const JoinArgs a) {
     __shared__ float sums[kParts][kJoinColumns];
     int row = blockIdx.y, which = 0;
     while (row >= a.rows[which]) row -= a.rows[which++];
-    const int column = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns, p = threadIdx.x / kJoinColumns;
+    const int p = threadIdx.x / kJoinColumns;
     const int64_t units = a.units[which];
-    const float* from = a.part[which] + int64_t(row) * units * a.hidden + column;
-    float s = 0.f;
-    if (column < a.hidden)
+    const float* const part = a.part[which] + int64_t(row) * units * a.hidden;
+    for (int first = blockIdx.x * kJoinColumns; first < a.hidden; first += gridDim.x * kJoinColumns) {
+        const int column = first + threadIdx.x % kJoinColumns;
+        float s = 0.f;
+        if (column < a.hidden)
 #pragma unroll 8
-        for (int64_t u = p; u < units; u += kParts) s += from[u * a.hidden];
-    sums[p][threadIdx.x % kJoinColumns] = s;
-    __syncthreads();
-    if (p == 0 && column < a.hidden) {
-        s = 0.f;
+            for (int64_t u = p; u < units; u += kParts) s += part[u * a.hidden + column];
+        sums[p][threadIdx.x % kJoinColumns] = s;
+        __syncthreads();
+        if (p == 0 && column < a.hidden) {
+            s = 0.f;
 #pragma unroll
-        for (int k = 0; k < kParts; ++k) s += sums[k][threadIdx.x];
-        if (a.f32[which]) static_cast<float*>(a.out[which])[int64_t(row) * a.hidden + column] = s;
-        else static_cast<TB*>(a.out[which])[int64_t(row) * a.hidden + column] = TB(s);
+            for (int k = 0; k < kParts; ++k) s += sums[k][threadIdx.x];
+            if (a.f32[which]) static_cast<float*>(a.out[which])[int64_t(row) * a.hidden + column] = s;
+            else static_cast<TB*>(a.out[which])[int64_t(row) * a.hidden + column] = TB(s);
+        }
+        __syncthreads();                             // the sums are the next columns'
     }
 }
 
@@ -62,7 +69,7 @@ public:
     // `dtype`: that of the outputs that are not fp32.
     fsdp_status run(fsdp_dtype dtype, hipStream_t stream) const {
         if (n_ == 0 || a_.hidden == 0) return FSDP_OK;
-        const dim3 grid(unsigned(ceil_div(a_.hidden, kJoinColumns)), unsigned(rows_));
+        const dim3 grid(unsigned(std::min(ceil_div(a_.hidden, kJoinColumns), kJoinGrid)), unsigned(rows_));
         return dtype == FSDP_DTYPE_BF16 ? launch(join_kernel<bf16>, a_, grid, kJoinThreads, stream)
                : dtype == FSDP_DTYPE_F16 ? launch(join_kernel<f16>, a_, grid, kJoinThreads, stream)
                                          : launch(join_kernel<float>, a_, grid, kJoinThreads, stream);

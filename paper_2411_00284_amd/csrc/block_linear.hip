@@ -212,20 +212,19 @@ struct Shape {
 
 // The most bytes that a load may lie from its tile's first (Operand::load), and
 // whether a form's loads stay within: an operand by rows has the tile's rows in a
-// step, one by columns the step's rows of k (all of them: past the last it reads
-// the zeros after the operand).  Without k nothing is loaded.
+// step, one by columns the step's rows of k.
 constexpr int64_t kReach = 0x7ffffff0;
 bool reaches(const Form& f, const Shape& s) {
-    if (s.k == 0) return true;
     const int64_t size = elem_bytes(s.dtype), deep = 128 / size;
     const auto end = [&](bool columns, int64_t rows, int64_t tile, int64_t stride) {
-        return columns ? ((deep - 1) * stride + tile) * size : (std::min(tile, rows) - 1) * stride * size + 128;
+        return columns ? ((std::min(deep, s.k) - 1) * stride + tile) * size : (std::min(tile, rows) - 1) * stride * size + 128;
     };
     return end(s.columns_a, s.m, f.tile_m, s.stride_a) <= kReach && end(s.columns_b, s.n, f.tile_n, s.stride_b) <= kReach;
 }
 
 constexpr int64_t kMostRows = 4;     // of row_kernel
-bool row_form(const Shape& s) { return s.m <= kMostRows && !s.columns_a && !s.columns_b; }
+// Below 2^27 columns: eight or sixteen of them to a workgroup must make fewer than 2^32 threads.
+bool row_form(const Shape& s) { return s.m <= kMostRows && s.n < (int64_t(1) << 27) && !s.columns_a && !s.columns_b; }
 
 // Bytes per us in which the operands come out of memory, in all and to one
 // workgroup, and what the caches keep of them: with the second bound, which wants

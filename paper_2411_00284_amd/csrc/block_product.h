@@ -238,6 +238,8 @@ struct Operand {
         return kSize == 4 ? (k >> 2 & 1) * 8 : kRows >= 128 ? (k & 3) * 4 : (k & 2) * 2;
     }
 
+    static constexpr int64_t kNowhere = 0xfffffff0u;   // out of any range
+
     const char* at;            // the step's first byte
     int64_t step;              // bytes from a step to the next
     int64_t left;              // bytes from `at` to the operand's end, in whole units
@@ -253,7 +255,7 @@ struct Operand {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int unit = (j * 4 + wave) * 64 + lane, kk = unit / kUnits, u = unit % kUnits;
-                offset[j] = uint32_t(kk * stride * kSize + (u ^ exchange(kk)) * 16);
+                offset[j] = uint32_t(min(kk * stride * kSize + (u ^ exchange(kk)) * 16, kNowhere));
             }
             k = 0;
         } else {
@@ -265,23 +267,24 @@ struct Operand {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int row = (j * 4 + wave) * 8 + lane / 8;
-                offset[j] = uint32_t(row * stride * kSize + u * 16);
+                offset[j] = uint32_t(min(row * stride * kSize + u * 16, kNowhere));
             }
         }
     }
 
     // Asks for the next step, with `rest` k left, into `lds`.  Offsets are 32 bits from
-    // the tile's first byte, and none passes kMost: the host takes no form of larger ones.
+    // the tile's first byte, and none of the operand's own passes kMost: the host takes no
+    // form of larger ones.
     __device__ __forceinline__ void load(char* lds, int64_t rest) {
         typedef __attribute__((address_space(3))) void lds_void;
-        constexpr uint32_t kMost = 0x7ffffff0u, kNowhere = 0xfffffff0u;
+        constexpr uint32_t kMost = 0x7ffffff0u;
         const uint32_t bytes = rest <= 0 ? 0u : uint32_t(min(left, int64_t(kMost)));
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, int(bytes), 0x00020000);
         const bool mine = kColumns || k < rest;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + (j * 4 + (threadIdx.x >> 6)) * 1024), 16,
-                                                     int(mine ? offset[j] : kNowhere), 0, 0, 0);
+                                                     int(mine ? offset[j] : uint32_t(kNowhere)), 0, 0, 0);
         at += step;
         left -= step;
     }
