@@ -221,6 +221,10 @@ fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args, void* work
  * valid entry, or whose valid v_k are all -inf, has loss 0, lse 0 and gradient
  * 0, whatever its logits hold.  p_k = 0 contributes 0.  A row with an id of
  * vocab or more has loss and gradient NaN.  A dloss of 0 gives a gradient of 0.
+ * Masked logits may be -inf or any finite value, over a part of a row or all of it
+ * (q and p are then uniform).  A saved lse is an fp32 value: the gradient from it is
+ * off by exp of its rounding, so that a row of logits that are all at such a mask
+ * has its gradient from fsdp_block_distill only.
  */
 #define FSDP_DISTILL_MAX_TOP 1024
 

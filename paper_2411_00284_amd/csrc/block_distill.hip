@@ -4,7 +4,7 @@
 // Bound by HBM: a row of logits is read for its maximum and sum (kept running
 // together, in one pass), and again for its gradient; a workgroup takes a row
 // and holds what it can of it in registers, so that the second read is of the
-// rest only, from cache.  Loss and gradient of 4096 x 128256 in bf16 take 435 us
+// rest only, from cache.  Loss and gradient of 4096 x 128256 in bf16 take 440 us
 // (4.8 TB/s of one read and one write).  The teacher's entries, at most 1024, lie
 // in LDS.
 
@@ -46,17 +46,21 @@ __device__ __forceinline__ int id_at(const DistillArgs& a, int64_t i) {
 // below the smallest normal number are 0.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The running maximum m and sum s of a softmax, over terms 2^(v c - m c) with
-// m c rounded: one multiply-add and one exponential a term.  A maximum of -inf
-// counts as 0 in the exponents, so that threads that hold nothing but -inf (or
-// nothing) keep a sum of 0.
+// The running maximum m and sum s of a softmax, over terms 2^((v - m) c): the
+// difference first, so that it is 0 at the maximum whatever its size (v c - m c as
+// one multiply-add leaves the rounding of m c, which at a mask of the type's lowest
+// value passes any exponent).  A maximum of -inf counts as 0 in the exponents, so
+// that threads that hold nothing but -inf (or nothing) keep a sum of 0.
 struct Softmax {
     float m = -INFINITY, s = 0.f;
-    __device__ static __forceinline__ float shift(float m, float c) { return m == -INFINITY ? 0.f : m * c; }
+    __device__ static __forceinline__ float base(float m) { return m == -INFINITY ? 0.f : m; }
+    // The sum s of maximum m over a maximum whose base is z; a sum of 0 stays one.
+    __device__ static __forceinline__ float moved(float s, float m, float z, float c) {
+        return s == 0.f ? 0.f : s * exp2_fast((m - z) * c);
+    }
     __device__ __forceinline__ void join(float m2, float s2, float c) {
-        const float top = fmaxf(m, m2), z = shift(top, c);
-        // A sum of 0 stays one, whatever its maximum.
-        s = (s == 0.f ? 0.f : s * exp2_fast(shift(m, c) - z)) + (s2 == 0.f ? 0.f : s2 * exp2_fast(shift(m2, c) - z));
+        const float top = fmaxf(m, m2), z = base(top);
+        s = moved(s, m, z, c) + moved(s2, m2, z, c);
         m = top;
     }
 };
@@ -107,13 +111,13 @@ __device__ __forceinline__ void add_units(Softmax& x, const Unit<T> (&u)[kUnits]
     for (int k = 0; k < kUnits; ++k)
 #pragma unroll
         for (int i = 0; i < Unit<T>::n; ++i) most = fmaxf(most, float(u[k].v[i]));
-    const float z = Softmax::shift(most, c);
-    if (most > x.m && x.s != 0.f) x.s *= exp2_fast(Softmax::shift(x.m, c) - z);
+    const float z = Softmax::base(most);
+    if (most > x.m) x.s = Softmax::moved(x.s, x.m, z, c);
     x.m = most;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k)
 #pragma unroll
-        for (int i = 0; i < Unit<T>::n; ++i) x.s += exp2_fast(float(u[k].v[i]) * c - z);
+        for (int i = 0; i < Unit<T>::n; ++i) x.s += exp2_fast((float(u[k].v[i]) - z) * c);
 }
 
 // f(entry, sum of p over the entries with its id).  Repeated ids are found
@@ -231,8 +235,8 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(co
             }
             x.join(lone, lone == -INFINITY ? 0.f : 1.f, c);
             // Over the wave: the maximum first, then sums of one shift.
-            const float m = wave_max(x.m), z = Softmax::shift(m, c);
-            x.s = wave_sum(x.s == 0.f ? 0.f : x.s * exp2_fast(Softmax::shift(x.m, c) - z));
+            const float m = wave_max(x.m);
+            x.s = wave_sum(Softmax::moved(x.s, x.m, Softmax::base(m), c));
             x.m = m;
         }
         __syncthreads();                                        // wm has been read
@@ -244,24 +248,27 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(co
         __syncthreads();
         sum = wave_sum(lane < kWaves ? wt[lane] : 0.f);
         if (!a.lse_in) {
-            const float m = wm[lane % kWaves], s1 = lane < kWaves ? ws[lane] : 0.f;
+            const float m = wm[lane % kWaves];
             x.m = wave_max(m);
-            x.s = wave_sum(s1 == 0.f ? 0.f : s1 * exp2_fast(Softmax::shift(m, c) - Softmax::shift(x.m, c)));
+            x.s = wave_sum(lane < kWaves ? Softmax::moved(ws[lane], m, Softmax::base(x.m), c) : 0.f);
         }
-        const double teacher = a.teacher_lse ? double(a.teacher_lse[row]) : double(top) * per_tau + log2_of(sum) * ln2;
-        // The rounding of m c, which the sum's terms had, is taken out of its logarithm.
-        const float lost = x.m == -INFINITY ? 0.f : fmaf(x.m, c, -Softmax::shift(x.m, c));
-        const double lse = a.lse_in ? double(a.lse_in[row]) : double(x.m) * per_tau + (log2_of(x.s) - double(lost)) * ln2;
-        if (t == 0 && a.lse) a.lse[row] = float(lse);
-        // p_k, their sum and the loss.
-        const float rest = float(teacher * tau - double(top));  // p_k = exp((v_k - top - rest) / tau)
+        // Both logarithms as log sums over their maxima, apart from these: of rows of one mask
+        // value the sum would be lost beside it.
+        const double log_sum = log2_of(x.s) * ln2;
+        if (t == 0 && a.lse) a.lse[row] = float(double(x.m) * per_tau + log_sum);
+        // p_k = exp((v_k - top) / tau - over) = exp((v_k - top - rest) / tau), their sum and the loss.
+        const double over = a.teacher_lse ? double(a.teacher_lse[row]) - double(top) * per_tau : log2_of(sum) * ln2;
+        const float rest = float(over * tau);
         float mass = 0.f;
         double loss = 0.0;
         if (some) {
             for (int k = t; k < a.top; k += kThreads) {
                 const float v = p[k], pk = exp2_fast(((v - top) - rest) * c);
                 mass += pk;
-                if (pk != 0.f) loss += double(pk) * ((double(v) - double(picked[k])) * per_tau - (teacher - lse));
+                // log p - log q
+                if (pk != 0.f)
+                    loss += double(pk) * (((double(v) - double(top)) * per_tau - over) -
+                                          ((double(picked[k]) - double(x.m)) * per_tau - log_sum));
                 p[k] = pk;
             }
             mass = wave_sum(mass);
@@ -282,12 +289,17 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(co
         }
         if (a.dlogits) {
             mass = wave_sum(lane < kWaves ? wp[lane] : 0.f);
-            // q = 2^(s c - b): b in two parts, the second as a factor
-            const double b = lse * tau * double(c);
-            const float base = float(b), scale = weight * a.tau;
+            // q = 2^((s - base) c) times what its base leaves: the sum over the row's maximum, or
+            // of a saved lse what float(lse tau) misses of it.
+            const float scale = weight * a.tau;
             const bool zero = weight == 0.f;
-            const float factor = scale * mass * exp2_fast(float(double(base) - b));
-            const auto slope = [&](float v) { return T(zero ? 0.f : factor * exp2_fast(v * c - base)); };
+            float base = Softmax::base(x.m), factor = scale * mass / x.s;
+            if (a.lse_in) {
+                const double b = double(a.lse_in[row]) * tau;
+                base = b > FLT_MAX ? FLT_MAX : b < -FLT_MAX ? -FLT_MAX : float(b);
+                factor = scale * mass * exp2_fast(float((double(base) - b) * double(c)));
+            }
+            const auto slope = [&](float v) { return T(zero ? 0.f : factor * exp2_fast((v - base) * c)); };
             const auto put = [&](const Unit<T>& u, int unit) {
                 if (unit >= units) return;
                 typename Unit<T>::vec out;
@@ -308,7 +320,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(co
             __syncthreads();                                    // the entries' places are written again
             if (!zero)                                          // the same for the whole workgroup
                 for_same_ids<kThreads>(a.top, ids, p, slots, [&](int k, float same) {
-                    ds[ids[k]] = T(factor * exp2_fast(picked[k] * c - base) - scale * same);
+                    ds[ids[k]] = T(factor * exp2_fast((picked[k] - base) * c) - scale * same);
                 });
         }
         __syncthreads();                                        // LDS is the next row's
