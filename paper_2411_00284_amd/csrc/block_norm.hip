@@ -243,9 +243,11 @@ __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const N
             flip ^= 1;
         }
         const float per = 1.f / float(hidden);
-        const float ry = a.dh ? rsqrtf(s[0] * per + a.eps) : 0.f, my = ry * ry * ry * (s[1] * per);
+        // The factors of u = y ry and n = branch rb.  Inverse roots meet what they normalise
+        // first: their cubes leave fp32's range for rows beyond 1e12, or (without eps) below 1e-12.
+        const float ry = a.dh ? rsqrtf(s[0] * per + a.eps) : 0.f, my = ry * (ry * (s[1] * per));
         const float rb = a.post ? rsqrtf(s[2] * per + a.eps) : 1.f;
-        const float mb = a.post ? rb * rb * rb * (a.branch_scale * (s[3] + ry * s[4] - my * s[5]) * per) : 0.f;
+        const float mb = a.post ? rb * (rb * (a.branch_scale * (s[3] + ry * s[4] - (ry * s[5]) * my) * per)) : 0.f;
         FSDP_CHUNKS(c, at, left) {
             if constexpr (!kRoomy) {
                 load_weights(c, at, left);
@@ -256,10 +258,10 @@ __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const N
             for (int i = 0; i < 8; ++i) {
                 g[i] = a.dy ? float(r.dy[c][i]) : 0.f;
                 if (a.dh) {
-                    const float up = float(r.dh[c][i]) * ry, y = float(r.y[c][i]);
-                    if constexpr (kRoomy) dpre[c][i] += up * y;
-                    else term[i] = up * y;
-                    g[i] += up * float(wy[c][i]) - y * my;
+                    const float d = float(r.dh[c][i]), u = float(r.y[c][i]) * ry;
+                    if constexpr (kRoomy) dpre[c][i] += d * u;
+                    else term[i] = d * u;
+                    g[i] += d * float(wy[c][i]) * ry - u * my;
                 }
             }
             if constexpr (!kRoomy)
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const N
                         else term[i] = dn * n;
                         dn *= float(wb[c][i]);
                     }
-                    g[i] = rb * dn - b * mb;
+                    g[i] = rb * dn - n * mb;
                 }
                 if constexpr (!kRoomy)
                     if (a.post) add_wide(1, c, term);
