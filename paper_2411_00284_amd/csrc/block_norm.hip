@@ -284,9 +284,9 @@ __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const N
                     if (a.post) {
                         if constexpr (kRoomy) dpost[c][i] += dn * n;
                         else term[i] = dn * n;
-                        dn *= float(wb[c][i]);
+                        dn = rb * (dn * float(wb[c][i])) - n * mb;
                     }
-                    g[i] = rb * dn - n * mb;
+                    g[i] = dn;                   // without post_weight the branch's values do not matter
                 }
                 if constexpr (!kRoomy)
                     if (a.post) add_wide(1, c, term);

@@ -4,6 +4,8 @@ form.  The squares of a row still add up within the range."""
 
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -39,3 +41,14 @@ def test_rows(hidden, block, scales, eps, with_dy):
     for k in want:
         close(got[k].t, want[k], bound[k], k)
         assert got[k].intact()
+
+
+def test_a_branch_without_its_norm():
+    """Without post_weight the branch is a summand: its gradient does not depend
+    on its values."""
+    t, n = 3, 500
+    dy, b, gate = normal(6, t, n), normal(2, t, n), normal(5, n)
+    b[0, 3], b[1, 4], b[2, 5] = math.inf, -math.inf, math.nan
+    out = torch.empty(t, n, device="cuda")
+    block_norm_backward(b.cuda(), dy=dy.cuda(), branch=b.cuda(), gate=gate.cuda(), dbranch=out, branch_scale=0.5)
+    assert torch.equal(out.cpu(), (0.5 * dy) * gate)
