@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
             for (int e = 0; e < 8; ++e) {
                 dz[e] = float(d[e]);
                 float value = 1.f, slope = 1.f;
-                if (a.pre) act_both(float(z[e]), a.act, value, slope);
+                if (a.pre) act_both<sizeof(T) == 4>(float(z[e]), a.act, value, slope);
                 df[e] = dz[e] * value;
                 if (a.times) dz[e] *= float(f[e]);
                 if (a.act != FSDP_ACT_NONE) dz[e] *= slope;

@@ -14,66 +14,96 @@ namespace {
 
 // ------------------------------------------------------------------ elementwise
 
-__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(1.44269504088896341f * x); }
-
-// To a few units of the last place: the hardware's exponential and reciprocal
-// take an eighth of the instructions of the rounded division and expf, which the
+// Exponentials and reciprocals are the hardware's, each to a unit of the last
+// place: an eighth of the instructions of the rounded division and expf, which the
 // gradient's elementwise pass would wait for instead of memory (4096 x 14336 with
-// SiLU: 133 us, with GELU by erfcf 191).
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-z)); }
+// SiLU: 133 us instead of 92, with GELU by erfcf 191).  What is below the smallest
+// normal number is 0.
+//
+// kFull (fp32): the exponent is held in two parts, and the activations are off by
+// some 12 units of 2^-24 of themselves (GELU's tanh form by the rounding of its
+// argument u more, 4 |u|).  Else the exponent's rounding stays in, |x| / 2 units more:
+// 7e-6 at GELU of -12, hundreds of times less than the rounding to 16 bits.
+template <bool kFull>
+__device__ __forceinline__ float exp_of(float x) {
+    constexpr float log2e = 1.44269504088896341f, rest = 1.9259629e-8f;      // rest: what log2e misses
+    const float hi = log2e * x, e = __builtin_amdgcn_exp2f(hi);
+    if constexpr (!kFull) return e;
+    const float lo = fmaf(x, rest, fmaf(x, log2e, -hi));
+    return fmaf(e, 0.69314718f * lo, e);
+}
+
+// 1 / (1 + exp(-z)), and that of -z, neither as a difference (kFull).
+template <bool kFull>
+__device__ __forceinline__ float sigmoid(float z, float* other) {
+    if constexpr (!kFull) {
+        const float q = __builtin_amdgcn_rcpf(1.f + exp_of<false>(-z));
+        *other = 1.f - q;
+        return q;
+    }
+    const float e = exp_of<true>(fmaxf(-fabsf(z), -150.f)), r = __builtin_amdgcn_rcpf(1.f + e);
+    *other = z < 0.f ? r : e * r;
+    return z < 0.f ? e * r : r;
+}
 
 // The normal distribution at z, and exp(-z^2 / 2).  erfc(x) = exp(-x^2) t P(t) with
 // t = 1 / (1 + 0.3 x) for x >= 0; P, of degree 8, is a minimax fit of the relative
 // error over x in [0, 10] (5e-7 as computed in fp32); past that erfc is 0 in fp32.
+template <bool kFull>
 __device__ __forceinline__ float normal_cdf(float z, float* bell) {
     constexpr float c[9] = {0.16918162f, 0.17081371f, 0.14769703f, 0.2172434f, -0.099725366f, 0.55464029f, -0.51802737f, 0.48822719f, -0.13005051f};
     const float t = __builtin_amdgcn_rcpf(1.f + 0.3f * 0.70710678118654752f * fabsf(z));
     float p = c[8];
 #pragma unroll
     for (int i = 7; i >= 0; --i) p = p * t + c[i];
-    *bell = exp_fast(-0.5f * z * z);
+    if constexpr (kFull) {
+        const float y = fminf(fabsf(z), 20.f), square = y * y, e = exp_of<true>(-0.5f * square);
+        *bell = fmaf(e, -0.5f * fmaf(y, y, -square), e);
+    } else {
+        *bell = exp_of<false>(-0.5f * z * z);
+    }
     const float tail = 0.5f * t * p * *bell;
     return z < 0.f ? tail : 1.f - tail;
 }
 
 // act(z); 1 + tanh(u) is 2 sigmoid(2u).
+template <bool kFull>
 __device__ __forceinline__ float act_value(float z, int act) {
+    float other;
     switch (act) {
         case FSDP_ACT_RELU: return z != z ? z : fmaxf(z, 0.f);
-        case FSDP_ACT_SILU: return z * sigmoid(z);
-        case FSDP_ACT_GELU: {
-            float bell;
-            return z * normal_cdf(z, &bell);
-        }
-        case FSDP_ACT_GELU_TANH: return z * sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
+        case FSDP_ACT_SILU: return z * sigmoid<kFull>(z, &other);
+        case FSDP_ACT_GELU: return z * normal_cdf<kFull>(z, &other);
+        case FSDP_ACT_GELU_TANH: return z * sigmoid<kFull>(1.5957691216057308f * (z + 0.044715f * z * z * z), &other);
         default: return z;
     }
 }
 
 // act(z) and its slope.
+template <bool kFull>
 __device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
+    float other;
     switch (act) {
         case FSDP_ACT_RELU:
             value = z != z ? z : fmaxf(z, 0.f);
             slope = z != z ? z : z > 0.f ? 1.f : 0.f;
             return;
         case FSDP_ACT_SILU: {
-            const float q = sigmoid(z);
+            const float q = sigmoid<kFull>(z, &other);
             value = z * q;
-            slope = q * (1.f + z * (1.f - q));
+            slope = q * (1.f + z * other);
             return;
         }
         case FSDP_ACT_GELU: {
-            float bell;
-            const float cdf = normal_cdf(z, &bell);
+            const float cdf = normal_cdf<kFull>(z, &other);
             value = z * cdf;
-            slope = cdf + z * (0.39894228040143268f * bell);
+            slope = cdf + z * (0.39894228040143268f * other);
             return;
         }
         case FSDP_ACT_GELU_TANH: {
-            const float q = sigmoid(1.5957691216057308f * (z + 0.044715f * z * z * z));
+            const float q = sigmoid<kFull>(1.5957691216057308f * (z + 0.044715f * z * z * z), &other);
             value = z * q;
-            slope = q + z * (q * (1.f - q)) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
+            slope = q + z * (q * other) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
             return;
         }
         default:
@@ -131,7 +161,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, int64_t i, int64_t j,
     if (e.pre) store_some(static_cast<T*>(e.pre) + i * e.pre_stride + j, left, z);
     if (e.act != FSDP_ACT_NONE)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[c] = act_value(z[c], e.act);
+        for (int c = 0; c < 8; ++c) z[c] = act_value<sizeof(T) == 4>(z[c], e.act);
     if (e.times)
 #pragma unroll
         for (int c = 0; c < 8; ++c) z[c] *= float(x.times[c]);
