@@ -103,7 +103,9 @@ __device__ __forceinline__ void act_both(float z, int act, float& value, float& 
         case FSDP_ACT_GELU_TANH: {
             const float q = sigmoid<kFull>(1.5957691216057308f * (z + 0.044715f * z * z * z), &other);
             value = z * q;
-            slope = q + z * (q * other) * (1.5957691216057308f * (1.f + 0.134145f * z * z));
+            // Past 30 the product of the two is 0, and z^2 may be infinite.
+            const float near = fminf(fabsf(z), 30.f);
+            slope = q + z * (q * other) * (1.5957691216057308f * (1.f + 0.134145f * near * near));
             return;
         }
         default:
