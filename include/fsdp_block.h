@@ -26,7 +26,8 @@
  *     Matrices of one row stride may interleave (column slices of one buffer).
  *   - Sums, statistics and products are held in fp32; each output is rounded
  *     once, to nearest even, unless a comment says otherwise.  Results do not
- *     depend on timing: no atomics, the same call gives the same bits.
+ *     depend on timing, the same call gives the same bits: sums are joined in a
+ *     fixed order, and nothing but counts of equal ids is atomic.
  *   - A call that needs scratch memory takes `workspace`, of at least the
  *     bytes its *_workspace query returns for the same arguments, 256-byte
  *     aligned; what it holds before the call does not matter, and it is free
@@ -61,7 +62,8 @@ const char* fsdp_block_last_error(void);
  *
  * gate has gate_rows rows; token t takes row t / (tokens / gate_rows):
  * gate_rows = 1 is one vector for all, the number of sequences a row for each
- * sequence, tokens a row for each token.
+ * sequence, tokens a row for each token.  (Without tokens the gradient takes at most
+ * 60000 rows.)
  */
 #define FSDP_NORM_MAX_HIDDEN 16384
 
@@ -133,7 +135,10 @@ fsdp_status fsdp_block_norm_grad(const fsdp_norm_grad_args* args, void* workspac
  *
  * x [m, k], weight [n, k] (a parameter as the copy-out leaves it), bias [n],
  * times, residual, pre and out [m, n], all of one type.  `pre` keeps z,
- * rounded, for the gradient; out is computed from z before that.
+ * rounded, for the gradient; out is computed from z before that.  Activations
+ * are off by some 12 units of 2^-24 of themselves in fp32 (GELU's tanh form by 4 of
+ * its argument more in its tail), by up to 7e-6 before the rounding to 16 bits; what
+ * takes an exponential below 2^-126 is 0.
  *
  * Sizes are at most 2^30, with 2^22 tiles of 64 x 64 in every matrix.  With more than
  * four rows of x, 64 rows of x and of weight (fp32: 64 and 128; all, if there are fewer)
@@ -230,7 +235,7 @@ fsdp_status fsdp_block_linear_grad(const fsdp_linear_grad_args* args, void* work
 
 typedef struct fsdp_distill_args {
     int64_t tokens;                /* >= 0 */
-    int64_t vocab;                 /* 1 .. 2^31 - 1 */
+    int64_t vocab;                 /* 1 .. 2^31 - 1 - 2^16 */
     int64_t top;                   /* 1 .. FSDP_DISTILL_MAX_TOP */
     fsdp_dtype dtype;              /* logits and dlogits */
     fsdp_dtype teacher_dtype;

@@ -118,6 +118,12 @@ struct SlopeArgs {
 // A workgroup takes 512 columns, eight per lane, of part_rows rows, one row per
 // wave at a time (two or four at a time: 5 to 10 % slower).  Bound by HBM: three
 // inputs and dtimes of 4096 x 14336 in bf16, with the sums, take 92 us (5.1 TB/s).
+//
+// dz is rounded to the type here, because the matrix instructions take factors of
+// 16 bits.  That is a rounding as large as the results' own: against 64 bits dx and
+// dweight of 4096 x 4096 -> 14336 are off by 2.3e-3 (2-norm, bf16) where the results'
+// rounding alone gives 1.7e-3.  Two 16-bit parts of dz would take it away for twice the
+// matrix work, which is nine tenths of the call.
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
     __shared__ float sums[4][512];
@@ -173,7 +179,9 @@ fsdp_status with_type(fsdp_dtype dtype, F f) {
 // The forms of a product in tiles.  Times in us of a step (64 k, fp32: 32) on one
 // MI355X: `alone` with one workgroup on a CU, `full` with `held` of them on every
 // CU, and `fixed` for the start and the end of a tile, as measured over products from
-// 16 x 14336 x 4096 to 8192 x 28672 x 8192 (fp32: 2048 x 1024 x 688 and 4096^3).
+// 16 x 14336 x 4096 to 8192 x 28672 x 8192.  A guide, not a prediction: 64 x 64 tiles
+// of 771 x 1153 x 2501 take 0.4 us a step.  Those of fp32 are from 2048 x 1024 x 688 and
+// 4096^3 only: dx of the former is expected at 24 us and takes 33.
 struct Form {
     int tile_m, tile_n, steps, held;
     double alone, full, fixed;

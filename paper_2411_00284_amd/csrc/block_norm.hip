@@ -6,9 +6,13 @@
 // statistics, the outputs) comes from there.  A row belongs to one team of
 // threads: a wave for short rows (four teams in a workgroup, no barrier), a
 // workgroup for longer ones.  8192 x 4096 in bf16 takes 55 us (4.9 TB/s); the
-// gradient of 8192 x 8192 with an fp32 stream, both weights and a gate 250 us (4.8
-// TB/s), 11 of them the join of the column sums.  Reads and writes past the caches
-// change that by -3 to 3 %, and reads cost 25 % at 32768 x 256.
+// gradient of 8192 x 8192 with an fp32 stream, both weights and a gate 251 us (4.8
+// TB/s), 12 of them the join of the column sums.
+//
+// Loads and stores go through the caches.  Past them (non-temporal) the forward at
+// 8192 x 4096 changes by 1 % and loses 25 % at 32768 x 256; an earlier form of the
+// gradient went from 99 to 92 us at 8192 x 4096 and from 282 to 238 at 4096 x 16384
+// (95 and 230 now, through the caches).
 
 #include "block_device.h"
 #include "block_host.h"
@@ -141,7 +145,7 @@ template <typename TX, typename TB, typename TW, int kTeam, int kChunks>
 __global__ __launch_bounds__(kTeam* kTeams<kTeam>) void norm_grad_kernel(const NormGradArgs a) {
     // 1024 threads have 128 registers each: two chunks leave no room for the next
     // row, the weights and the weights' sums, which then lie in LDS (in registers
-    // they spilled: 855 instead of 282 us at 4096 x 16384).
+    // they spilled: 855 us at 4096 x 16384, which takes 230 so).
     constexpr bool kRoomy = kTeam < 1024 || kChunks == 1;
     constexpr int kGroup = kTeams<kTeam>;
     __shared__ float part[2][6 * (kTeam / 64)];
