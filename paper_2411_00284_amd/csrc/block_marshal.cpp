@@ -165,6 +165,12 @@ PyObject* entry(Py_ssize_t n, Py_ssize_t want, F f) {
     try {
         return PyLong_FromLong(f());
     } catch (const Raised&) {
+    } catch (const c10::OutOfMemoryError& e) {                   // of the workspace, as torch raises it
+        PyObject* const torch = PyImport_ImportModule("torch");
+        PyObject* const type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (type) PyErr_SetString(type, e.what_without_backtrace());
+        Py_XDECREF(type);
+        Py_XDECREF(torch);
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     } catch (...) {
