@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void distill_kernel(co
     __shared__ double wd[kWaves];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, vocab = a.vocab, units = vocab / n;
     const int single = units * n + t;                           // this thread's element after the units
-    const float c = kLog2e / a.tau;
+    const float c = fminf(kLog2e / a.tau, FLT_MAX);             // finite for a subnormal tau: 0 c is 0
     const double tau = double(a.tau), per_tau = 1.0 / tau, ln2 = 0.6931471805599453;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         const T* const s = static_cast<const T*>(a.logits) + row * a.logits_stride;

@@ -122,3 +122,25 @@ def test_masked(dtype, low, form, tau):
     distill_loss_backward(gd, gl, gt, gi, lse, back, temperature=tau)
     _, _, wg, _, _, eg = reference(logits[saved], teacher[saved], ids[saved], tau, dloss[saved], lse[:n].cpu()[saved])
     close(back[:n][saved.cuda()], wg, eg, "dlogits from lse")
+
+
+@pytest.mark.parametrize("tau", [1e-3, 1e-20, 1e-30, 2.0 ** -126, 2.0 ** -140])
+@pytest.mark.parametrize("vocab", [2003, 20011])
+def test_small_temperatures(tau, vocab):
+    """q and p go over to one hot; tau is subnormal at last."""
+    tau = torch.tensor(tau).item()
+    n = 5
+    logits = normal(3, n, vocab).round(decimals=1)
+    logits[:, 17] = 9.0                                        # the largest by a margin
+    logits[1, 18] = 9.0                                        # a tie
+    teacher = normal(4, n, TOP).round(decimals=1)
+    teacher[:, 5] = 8.0
+    ids = torch.randint(20, vocab, (n, TOP), generator=torch.Generator().manual_seed(1))
+    ids[:, 5] = 17
+    ids[2, 5] = 30                                             # the teacher's choice is not the student's
+    dloss = torch.ones(n) / tau if tau > 1e-25 else torch.ones(n)
+    loss, dl = torch.empty(n, device="cuda"), torch.empty(n, vocab, device="cuda")
+    distill_loss(logits.cuda(), teacher.cuda(), ids.cuda(), loss, temperature=tau, dloss=dloss.cuda(), dlogits=dl)
+    wl, _, wg, el, _, eg = reference(logits, teacher, ids, tau, dloss)
+    close(loss, wl, el, "loss")
+    close(dl, wg, eg, "dlogits")
