@@ -19,7 +19,9 @@ void clear_error();
 int cu_count(fsdp_status* st);
 
 inline bool known_dtype(fsdp_dtype t) { return t == FSDP_DTYPE_BF16 || t == FSDP_DTYPE_F32 || t == FSDP_DTYPE_F16; }
-inline int elem_bytes(fsdp_dtype t) { return t == FSDP_DTYPE_F32 ? 4 : 2; }
+// Of a Matrix of single bytes (codes and scales); no call takes it.
+constexpr fsdp_dtype kBytes = 1 << 8;
+inline int elem_bytes(fsdp_dtype t) { return t == FSDP_DTYPE_F32 ? 4 : t == kBytes ? 1 : 2; }
 
 // One matrix argument of a call.
 struct Matrix {

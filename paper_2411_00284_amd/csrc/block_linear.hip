@@ -9,8 +9,10 @@
 // With few tiles the sum over k is cut into parts, which join_parts_kernel joins
 // in order; with many, a last round of few tiles is a launch of its own.
 
-#include "block_product.h"
+#include "block_cut.h"
 #include "block_join.h"
+#include "block_lay.h"
+#include "block_product.h"
 
 #include <algorithm>
 
@@ -66,42 +68,6 @@ __global__ __launch_bounds__(256) void row_kernel(const Product p) {
                 float z[8] = {sum[o][i]};
                 if (j0 + o < p.n) finish8<T>(p.e, i, j0 + o, 1, z);
             }
-}
-
-// ------------------------------------------------------------------ onto the grid
-
-// Copies matrices to rows of whole lines, zeros after their columns up to a whole
-// 16-byte unit.  Sizes in halves of 32 bits, which fp32 elements are two of.  A
-// wave takes 64 units of a row, so that the division is one for all of them.
-struct PadArgs {
-    const uint16_t* from[2];
-    uint16_t* to[2];
-    int64_t rows[2], cols[2], stride[2], to_stride[2];
-    uint32_t runs[2];                // of 64 units, in a row
-};
-
-__global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
-    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-    struct __attribute__((packed, aligned(2))) any {
-        u16x8 v;
-    };
-    const uint32_t first = uint32_t(a.rows[0]) * a.runs[0], all = first + uint32_t(a.rows[1]) * a.runs[1];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
-    for (uint32_t item = wave; item < all; item += gridDim.x * 4) {
-        const int which = item >= first;
-        const uint32_t run = which ? item - first : item, row = run / a.runs[which];
-        const int64_t j = (int64_t(run - row * a.runs[which]) * 64 + threadIdx.x % 64) * 8, left = a.cols[which] - j;
-        if (left <= 0) continue;
-        const uint16_t* at = a.from[which] + row * a.stride[which] + j;
-        u16x8 v;
-        if (left >= 8) {
-            v = reinterpret_cast<const any*>(at)->v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < left ? at[e] : uint16_t(0);
-        }
-        *reinterpret_cast<u16x8*>(a.to[which] + row * a.to_stride[which] + j) = v;
-    }
 }
 
 // ------------------------------------------------------------------ dz
@@ -171,173 +137,6 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
 
 // ------------------------------------------------------------------ host side
 
-template <typename F>
-fsdp_status with_type(fsdp_dtype dtype, F f) {
-    return dtype == FSDP_DTYPE_BF16 ? f(bf16(0.f)) : dtype == FSDP_DTYPE_F16 ? f(f16(0.f)) : f(0.f);
-}
-
-// The forms of a product in tiles.  Times in us of a step (64 k, fp32: 32) on one
-// MI355X: `alone` with one workgroup on a CU, `full` with `held` of them on every
-// CU, and `fixed` for the start and the end of a tile, as measured over products from
-// 16 x 14336 x 4096 to 8192 x 28672 x 8192.  A guide, not a prediction: 64 x 64 tiles
-// of 771 x 1153 x 2501 take 0.4 us a step.  Those of fp32 are from 2048 x 1024 x 688 and
-// 4096^3 only: dx of the former is expected at 24 us and takes 33.
-struct Form {
-    int tile_m, tile_n, steps, held;
-    double alone, full, fixed;
-};
-constexpr Form kForms16[] = {
-    {256, 256, 2, 1, 1.15, 1.60, 6.0},
-    {128, 128, 2, 2, 0.60, 0.97, 4.0},
-    {128, 128, 4, 1, 0.36, 0.52, 3.5},
-    {64, 128, 4, 1, 0.25, 0.32, 3.5},
-    {64, 64, 8, 1, 0.14, 0.20, 3.5},
-};
-constexpr Form kForms32[] = {
-    {128, 128, 2, 2, 1.80, 3.60, 4.0},
-    {64, 128, 4, 1, 0.95, 0.95, 3.5},
-};
-
-// How one product is run.
-struct Cut {
-    const Form* form = nullptr;      // NULL: row_kernel
-    int count = 1;                   // parts of k
-    int64_t part_k = 0;
-    // Not NULL: the rows (columns) of out from rest_at on are a launch of their own.
-    const Form* rest = nullptr;
-    bool rest_rows = false;
-    int64_t rest_at = 0;
-    // Byte offsets in the workspace and its size: the operands laid on the grid, the parts.
-    int64_t pad_a = -1, pad_b = -1, parts = -1, bytes = 0;
-};
-
-struct Shape {
-    int64_t m, n, k;
-    fsdp_dtype dtype;
-    bool columns_a, columns_b;
-    int64_t stride_a, stride_b;      // of the operands as they are laid on the grid
-};
-
-// The most bytes that a load may lie from its tile's first (Operand::load), and
-// whether a form's loads stay within: an operand by rows has the tile's rows in a
-// step, one by columns the step's rows of k.
-constexpr int64_t kReach = 0x7ffffff0;
-bool reaches(const Form& f, const Shape& s) {
-    const int64_t size = elem_bytes(s.dtype), deep = 128 / size;
-    const auto end = [&](bool columns, int64_t rows, int64_t tile, int64_t stride) {
-        return columns ? ((std::min(deep, s.k) - 1) * stride + tile) * size : (std::min(tile, rows) - 1) * stride * size + 128;
-    };
-    return end(s.columns_a, s.m, f.tile_m, s.stride_a) <= kReach && end(s.columns_b, s.n, f.tile_n, s.stride_b) <= kReach;
-}
-
-constexpr int64_t kMostRows = 4;     // of row_kernel
-// Below 2^27 columns: eight or sixteen of them to a workgroup must make fewer than 2^32 threads.
-bool row_form(const Shape& s) { return s.m <= kMostRows && s.n < (int64_t(1) << 27) && !s.columns_a && !s.columns_b; }
-
-// Bytes per us in which the operands come out of memory, in all and to one
-// workgroup, and what the caches keep of them: with the second bound, which wants
-// 220 workgroups, 64 x 14336 -> 4096 takes 29.5 us instead of 45, 64 x 28672 -> 8192
-// 104 instead of 140; under 16 MB it would cut products for nothing (64 x 1024 -> 1024
-// 9.1 us instead of 7.2).
-constexpr double kMostRead = 5.5e6, kGroupRead = 0.025e6, kCached = 16e6;
-
-// Of whole rounds of workgroups and the last one.
-double rounds_time(const Form& form, int64_t groups, int64_t steps, int cus) {
-    const int64_t slots = int64_t(cus) * form.held, whole = groups / slots, rest = groups - whole * slots;
-    const double time = double(whole) * (double(steps) * form.full + form.fixed);
-    return rest ? time + double(steps) * (rest > cus ? form.full : form.alone) + form.fixed : time;
-}
-
-// The form and the cut with the least expected time: whole rounds of workgroups
-// over the CUs, the fullest CU of the last round, reading the operands if that takes
-// longer, and the join of the parts (3 us, and 8 bytes moved per value and part).
-// Up to four rows of x, row_kernel reads the weight at HBM's rate in one launch.
-// Tiles of 256 x 256 that leave a last round of few are cut where the whole rounds
-// end, and the rest of out takes tiles of 128 x 128 in a second launch (3 us): bf16
-// 6144 x 6144 x 4096 takes 281 us instead of 301, 14336 x 4096 with k = 8192 746
-// instead of 791.  (Smaller tiles for the rest: 334 instead of 300 us at 5000^3.)
-Cut choose(const Shape& s, int cus) {
-    Cut best;
-    if (row_form(s)) return best;
-    const bool wide = s.dtype == FSDP_DTYPE_F32;
-    const Form* const forms = wide ? kForms32 : kForms16;
-    const int step_k = wide ? 32 : 64;
-    const int64_t steps = std::max<int64_t>(1, ceil_div(s.k, step_k));
-    const double read = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k));
-    const double joining = double(s.m) * double(s.n) * 8 / 5e6;
-    double least = 0;
-    for (int f = 0; f < (wide ? 2 : 5); ++f) {
-        const Form& form = forms[f];
-        if (!reaches(form, s)) continue;
-        const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n);
-        for (int parts = 1; parts <= 16; ++parts) {
-            // Parts of at least four steps, and no more of them than some rounds.
-            if (parts > 1 && (steps < 4 * parts || tiles * (parts - 1) > 3 * int64_t(cus))) break;
-            const int64_t each = (steps + parts - 1) / parts, count = (steps + each - 1) / each;
-            if (count != parts) continue;
-            const int64_t groups = tiles * parts;
-            double time = rounds_time(form, groups, each, cus);
-            const double rate = read > kCached ? std::min(kMostRead, kGroupRead * double(groups)) : kMostRead;
-            time = std::max(time, read / rate + form.fixed);
-            if (parts > 1) time += 3.0 + double(parts) * joining;
-            if (!best.form || time < least) {
-                least = time;
-                best.form = &form;
-                best.part_k = each * step_k;
-                best.count = parts;
-            }
-        }
-    }
-    if (wide || s.m == 0 || s.n == 0) return best;
-    const Form &big = forms[0], &small = forms[1];
-    if (!reaches(big, s)) return best;
-    const int64_t down = ceil_div(s.m, big.tile_m), across = ceil_div(s.n, big.tile_n);
-    for (const bool rows : {true, false}) {
-        // Rows (columns) of tiles in whole rounds, and what is left of out.
-        const int64_t other = rows ? across : down, taken = down * across / cus * cus / other;
-        const int64_t at = taken * (rows ? big.tile_m : big.tile_n), m = rows ? s.m - at : s.m, n = rows ? s.n : s.n - at;
-        if (taken == 0 || m <= 0 || n <= 0) continue;
-        const double time = rounds_time(big, taken * other, steps, cus) + 3.0 +
-                            rounds_time(small, ceil_div(m, small.tile_m) * ceil_div(n, small.tile_n), steps, cus);
-        if (time >= least) continue;
-        least = time;
-        best = Cut{};
-        best.form = &big;
-        best.part_k = steps * step_k;
-        best.rest = &small;
-        best.rest_rows = rows;
-        best.rest_at = at;
-    }
-    return best;
-}
-
-struct Source {
-    const void* p;
-    int64_t rows, cols, stride;      // as it lies in memory
-    bool zeros;                      // zeros follow a row, up to a whole 16-byte unit
-};
-
-// Elements of a row laid out in whole lines.
-int64_t lined(int64_t cols, fsdp_dtype dtype) { return round_up(cols, 128 / elem_bytes(dtype)); }
-
-// Whether an operand lies on the 16-byte grid in whole units, as product_kernel
-// reads it, with the offsets of a step in 31 bits.
-bool on_grid(const Source& o, fsdp_dtype dtype) {
-    const int unit = 16 / elem_bytes(dtype);
-    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.stride % unit == 0 && o.stride < (1 << 21) && (o.zeros || o.cols % unit == 0);
-}
-
-// A row's stride where product_kernel reads it.
-int64_t laid_stride(const Source& o, fsdp_dtype dtype) { return on_grid(o, dtype) ? o.stride : lined(o.cols, dtype); }
-
-// Whether any form reaches the operands (row_kernel reaches all of its).
-fsdp_status check_reach(const Shape& s) {
-    if (s.m == 0 || s.n == 0 || row_form(s)) return FSDP_OK;
-    if (s.dtype == FSDP_DTYPE_F32 ? reaches(kForms32[1], s) : reaches(kForms16[4], s)) return FSDP_OK;
-    return fail(FSDP_ERR_OVERFLOW, "a tile's rows of an operand of %lld x %lld, %lld x %lld do not lie within 2^31 bytes",
-                (long long)s.m, (long long)s.k, (long long)s.n, (long long)s.k);
-}
-
 // Adds a product's needs to those of `bytes`.
 Cut plan(const Shape& s, const Source& a, const Source& b, int cus, int64_t bytes) {
     Cut c = choose(s, cus);
@@ -391,29 +190,16 @@ fsdp_status run_product(const Shape& s, const Source& a, const Source& b, const 
         });
     }
     fsdp_status st;
-    if (c.pad_a >= 0 || c.pad_b >= 0) {
-        PadArgs pad{};
-        const int halves = elem_bytes(s.dtype) / 2;
-        const auto lay = [&](int which, const Source& o, int64_t at, const void** to, int64_t* stride) {
-            pad.runs[which] = 1;
-            if (at < 0) return;
-            pad.from[which] = static_cast<const uint16_t*>(o.p);
-            pad.to[which] = reinterpret_cast<uint16_t*>(ws + at);
-            pad.rows[which] = o.rows;
-            pad.cols[which] = o.cols * halves;
-            pad.stride[which] = o.stride * halves;
-            pad.to_stride[which] = lined(o.cols, s.dtype) * halves;
-            pad.runs[which] = uint32_t(ceil_div(pad.cols[which], 512));
-            *to = ws + at;
-            *stride = lined(o.cols, s.dtype);
-        };
-        lay(0, a, c.pad_a, &p.a, &p.a_stride);
-        lay(1, b, c.pad_b, &p.b, &p.b_stride);
-        const int64_t runs = pad.rows[0] * pad.runs[0] + pad.rows[1] * pad.runs[1];
-        // check_sizes bounds rows x cols by 2^34 and rows by 2^28: the runs fit 31 bits.
-        if ((st = launch(pad_kernel, pad, dim3(unsigned(std::min<int64_t>(ceil_div(runs, 4), 1 << 16))), 256, stream)) != FSDP_OK)
-            return st;
-    }
+    Pads<2> pads;
+    const auto lay = [&](const Source& o, int64_t at, const void** to, int64_t* stride) {
+        if (at < 0) return;
+        pads.add(o, s.dtype, ws + at);
+        *to = ws + at;
+        *stride = lined(o.cols, s.dtype);
+    };
+    lay(a, c.pad_a, &p.a, &p.a_stride);
+    lay(b, c.pad_b, &p.b, &p.b_stride);
+    if ((st = pads.run(stream)) != FSDP_OK) return st;
     p.part_k = c.part_k;
     p.count = c.count;
     p.parts = c.parts < 0 ? nullptr : reinterpret_cast<float*>(ws + c.parts);

@@ -330,8 +330,11 @@ struct LaneUnit {
 
 // A wave's registers of half a step: kTiles times 32 rows of an operand, in two
 // pairs of units.
-template <typename T, int kRows, bool kColumns, int kTiles>
+// (kApart: how many rows lie between the first half of the tiles and the second, over
+// what they cover: 0 where they follow each other.)
+template <typename T, int kRows, bool kColumns, int kTiles, int kApart = 0>
 struct Fragments {
+    static constexpr int row_of(int x) { return x * 32 + (x >= kTiles / 2 ? kApart : 0); }
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr int kPlaces = kColumns ? kTiles : 4;
     static constexpr int kReads = 2 * kTiles * (!kColumns ? 1 : kWide ? 4 : 2);     // LDS instructions
@@ -359,7 +362,7 @@ struct Fragments {
 #pragma unroll
             for (int x = 0; x < kTiles; ++x) {
                 if constexpr (!kColumns) {
-                    v[h][x] = *reinterpret_cast<const typename LaneUnit<T>::type*>(lds + place[2 * half + h] + x * 32 * 128);
+                    v[h][x] = *reinterpret_cast<const typename LaneUnit<T>::type*>(lds + place[2 * half + h] + row_of(x) * 128);
                 } else if constexpr (kWide) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -375,10 +378,27 @@ struct Fragments {
     }
 };
 
-template <typename T, bool kColumnsA, bool kColumnsB, int kTileM, int kTileN, int kSteps>
-__global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void product_kernel(const Product p) {
-    using A = Operand<T, kTileM, kColumnsA>;
+// What a kind of product has of its own: where B lies, how far apart the columns of a
+// wave's tiles are, and what becomes of eight columns of a row.  This is the kind of one
+// matrix B and one of out.
+struct OneMatrix {
+    static constexpr bool kPair = false;         // tiles of kTileN / 2 columns of two matrices
+    template <typename T, int kTileN, bool kColumnsB>
     using B = Operand<T, kTileN, kColumnsB>;
+    template <typename T, int kTileN, bool kColumnsB>
+    __device__ static __forceinline__ auto operand(const Product& p, int64_t j0, int64_t k0, int64_t k1) {
+        return B<T, kTileN, kColumnsB>(p.b, p.b_stride, j0, p.n, k0, k1);
+    }
+    template <typename T>
+    __device__ static __forceinline__ void store(const Product& p, int64_t i, int64_t j, int left, const float (&z)[8]) {
+        store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
+    }
+};
+
+template <typename T, bool kColumnsA, bool kColumnsB, int kTileM, int kTileN, int kSteps, typename Kind, typename Args>
+__device__ __forceinline__ void product_tile(const Args& p) {
+    using A = Operand<T, kTileM, kColumnsA>;
+    using B = typename Kind::template B<T, kTileN, kColumnsB>;
     constexpr int kDeep = A::kDeep;
     constexpr int kA = kTileM / 64, kB = kTileN / 64;            // 32-row tiles of a wave
     // One array per step: their reads and loads are known not to touch each other.
@@ -394,14 +414,14 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
     const int64_t i0 = p.first_i + int64_t(t.row) * kTileM, j0 = p.first_j + int64_t(t.column) * kTileN;
     const int64_t k0 = t.part * p.part_k, k1 = min(k0 + p.part_k, p.k);
     A a(p.a, p.a_stride, i0, p.m, k0, k1);
-    B b(p.b, p.b_stride, j0, p.n, k0, k1);
+    B b = Kind::template operand<T, kTileN, kColumnsB>(p, j0, k0, k1);
     using FA = Fragments<T, kTileM, kColumnsA, kA>;
-    using FB = Fragments<T, kTileN, kColumnsB, kB>;
+    using FB = Fragments<T, kTileN, kColumnsB, kB, Kind::kPair ? kTileN / 4 : 0>;
     FA fa[2];
     FB fb[2];
     int pa[FA::kPlaces], pb[FB::kPlaces];
     FA::lane_places(wi, pa);
-    FB::lane_places(wj, pb);
+    FB::lane_places(Kind::kPair ? wj / 2 : wj, pb);
     f32x16 acc[kA][kB] = {};
 
     // Waits for this wave's loads, but for those of the last kLater steps, and
@@ -513,6 +533,26 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
                                     : (wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? b0 : b1);
     float* const turn = reinterpret_cast<float*>(piece);
     const auto place = [](int row, int column) { return row * kWide + (column ^ (kWide > 32 ? row / 4 % 2 * 32 : 0)); };
+    if constexpr (Kind::kPair) {
+        Kind::template finish<T, kWide>(p, t.part, turn, place, i0 + wi, (j0 + wj) / 2, [&](auto each) {
+#pragma unroll
+            for (int x0 = 0; x0 < kA; x0 += kTurn) {
+#pragma unroll
+                for (int x = 0; x < kTurn; ++x)
+#pragma unroll
+                    for (int y = 0; y < kB; ++y)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            turn[place(32 * x + 8 * (r / 4) + 4 * (lane / 32) + r % 4, 32 * y + lane % 32)] = acc[x0 + x][y][r];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                each(32 * x0, 32 * kTurn);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        });
+        return;
+    }
     const int column = lane % kLanes * 8;
     const int64_t j = j0 + wj + column;
     const int left = int(min(p.n - j, int64_t(8)));
@@ -547,7 +587,7 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
                 if (p.count > 1) {
                     store_some(p.parts + (t.part * p.m + i) * ((p.n + 7) / 8 * 8) + j, 8, z);
                 } else if constexpr (kColumnsB) {                 // dx and dweight have no epilogue
-                    store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
+                    Kind::template store<T>(p, i, j, left, z);
                 } else {
                     finish8<T>(p.e, i, j, left, bias, extra[u], z);
                 }
@@ -556,6 +596,14 @@ __global__ __launch_bounds__(256, (kTileM + kTileN) * kSteps > 512 ? 1 : 2) void
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <int kTileM, int kTileN, int kSteps>
+constexpr int kTilesPerCu = (kTileM + kTileN) * kSteps > 512 ? 1 : 2;
+
+template <typename T, bool kColumnsA, bool kColumnsB, int kTileM, int kTileN, int kSteps>
+__global__ __launch_bounds__(256, (kTilesPerCu<kTileM, kTileN, kSteps>)) void product_kernel(const Product p) {
+    product_tile<T, kColumnsA, kColumnsB, kTileM, kTileN, kSteps, OneMatrix>(p);
 }
 
 }  // namespace
