@@ -16,6 +16,7 @@ import torch  # noqa: F401  (must precede the library: shared HIP runtime)
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfsdp_bucket.so")
 BLOCK_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfsdp_block.so")
+STEP_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfsdp_step.so")
 
 c_status = ctypes.c_int32
 c_plan_p = ctypes.c_void_p
@@ -143,3 +144,15 @@ def load_block():
         raise ImportError(f"two HIP runtimes are mapped ({sorted(runtimes)}); "
                           "import torch before loading libfsdp_block.so")
     return _block_marshal
+
+
+def load_step():
+    """The marshaller of the operators of ``step`` (csrc/step_marshal.cpp), which
+    links ``libfsdp_step.so`` beside it."""
+    load_block()
+    try:
+        from . import _step_marshal
+    except ImportError as e:
+        raise ImportError(f"the step's operators do not load ({e}): run "
+                          "`python -m paper_2411_00284_amd.build` first; there is no fallback path") from e
+    return _step_marshal

@@ -102,7 +102,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, *, bias=Non
     _check(_lib().linear(x, weight, out, bias, _activation(activation), times, residual, pre, stream), "fsdp_block_linear")
 
 
-def linear_backward(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *, activation=None, pre=None, times=None,
+def linear_backward(dout: torch.Tensor, x, weight: torch.Tensor, *, activation=None, pre=None, times=None,
                     dx=None, dweight=None, dbias=None, dtimes=None, stream=None) -> None:
     """The gradient of ``linear`` from that of its output:
 
@@ -112,7 +112,11 @@ def linear_backward(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *
 
     Writes the outputs that are given.  ``pre`` is what ``linear`` wrote there;
     it is needed with an activation and for ``dtimes`` (which may be
-    ``times``)."""
+    ``times``).  ``x`` and ``pre`` may each be a ``step.Checkpoint``."""
+    if isinstance(x, tuple) or isinstance(pre, tuple):
+        from . import step
+        return step._check(step._lib().linear_grad(dout, x, weight, _activation(activation), pre, times, dx, dweight, dbias, dtimes,
+                                                   stream), "fsdp_step_linear_grad")
     _check(_lib().linear_grad(dout, x, weight, _activation(activation), pre, times, dx, dweight, dbias, dtimes, stream),
            "fsdp_block_linear_grad")
 

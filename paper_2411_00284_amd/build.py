@@ -38,6 +38,11 @@ BLOCK_LIB_NAME = "libfsdp_block.so"
 BLOCK_LIB_PATH = os.path.join(PKG, BLOCK_LIB_NAME)
 BLOCK_MARSHAL_PATH = os.path.join(PKG, "_block_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
+# The operators of fsdp_step.h: a library that links the block operators' one, and its marshaller.
+STEP_LIB_NAME = "libfsdp_step.so"
+STEP_LIB_PATH = os.path.join(PKG, STEP_LIB_NAME)
+STEP_MARSHAL_PATH = os.path.join(PKG, "_step_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
@@ -53,6 +58,7 @@ HOST_SOURCES = ["plan.cpp", "auto_wrap.cpp"]
 BLOCK_FLAGS = [f if f != "-ffp-contract=off" else "-ffp-contract=fast" for f in DEVICE_FLAGS]
 BLOCK_SOURCES = ["block_norm.hip", "block_linear.hip", "block_distill.hip"]
 BLOCK_HOST_SOURCES = ["block_host.cpp"]
+STEP_SOURCES = ["step_gated.hip", "step_saved.hip", "step_policy.hip"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-ffp-contract=off", "-D__HIP_PLATFORM_AMD__"]
 
 
@@ -89,6 +95,7 @@ def build(verbose: bool = False, defines=(), out_dir: str | None = None) -> str:
         return lib_path
     _build_marshal(verbose)
     build_block(verbose)
+    build_step(verbose)
     pobj = os.path.join(BUILD, "ceiling_probes.o")
     _run([HIPCC, *DEVICE_FLAGS, *inc, "-c", os.path.join(CSRC, "ceiling_probes.hip"), "-o", pobj], verbose)
     tmp = PROBES_PATH + f".tmp{os.getpid()}"
@@ -100,8 +107,27 @@ def build(verbose: bool = False, defines=(), out_dir: str | None = None) -> str:
 def build_block(verbose: bool = False, out_dir: str | None = None) -> str:
     """Compile the block operators' library; returns its path.  With
     ``out_dir``, the library alone, into that folder."""
+    lib_path = _build_library(BLOCK_LIB_NAME, [*BLOCK_SOURCES, *BLOCK_HOST_SOURCES], [], verbose, out_dir)
+    if out_dir is None:
+        _build_extension("block_marshal.cpp", BLOCK_MARSHAL_PATH, verbose,
+                         [f"-L{PKG}", "-lfsdp_block", "-Wl,-rpath,$ORIGIN"])
+    return lib_path
+
+
+def build_step(verbose: bool = False, out_dir: str | None = None) -> str:
+    """As ``build_block``, the library of ``fsdp_step.h``, which links that one
+    (beside it)."""
+    lib_path = _build_library(STEP_LIB_NAME, STEP_SOURCES, [f"-L{out_dir or PKG}", "-lfsdp_block", "-Wl,-rpath,$ORIGIN"], verbose,
+                              out_dir)
+    if out_dir is None:
+        _build_extension("step_marshal.cpp", STEP_MARSHAL_PATH, verbose,
+                         [f"-L{PKG}", "-lfsdp_step", "-lfsdp_block", "-Wl,-rpath,$ORIGIN"])
+    return lib_path
+
+
+def _build_library(name: str, sources, link, verbose: bool, out_dir: str | None) -> str:
     bdir = os.path.join(out_dir, "_build") if out_dir else BUILD
-    lib_path = os.path.join(out_dir, BLOCK_LIB_NAME) if out_dir else BLOCK_LIB_PATH
+    lib_path = os.path.join(out_dir or PKG, name)
     os.makedirs(bdir, exist_ok=True)
     inc = [f"-I{INCLUDE}", f"-I{CSRC}", f"-I{os.path.join(ROCM, 'include')}"]
 
@@ -112,13 +138,10 @@ def build_block(verbose: bool = False, out_dir: str | None = None) -> str:
         return obj
 
     with ThreadPoolExecutor(4) as pool:
-        objs = list(pool.map(compile_one, [*BLOCK_SOURCES, *BLOCK_HOST_SOURCES]))
+        objs = list(pool.map(compile_one, sources))
     tmp = lib_path + f".tmp{os.getpid()}"
-    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", f"-Wl,-soname,{BLOCK_LIB_NAME}", "-o", tmp, *objs], verbose)
+    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", f"-Wl,-soname,{name}", "-o", tmp, *objs, *link], verbose)
     os.replace(tmp, lib_path)
-    if out_dir is None:
-        _build_extension("block_marshal.cpp", BLOCK_MARSHAL_PATH, verbose,
-                         [f"-L{PKG}", "-lfsdp_block", "-Wl,-rpath,$ORIGIN"])
     return lib_path
 
 

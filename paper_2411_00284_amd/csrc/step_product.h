@@ -1,0 +1,234 @@
+// Matrix products over two weights that share their input (block_product.h has
+// the tiles): a gated feed-forward's forward product, and the gradients of its
+// input and of its weights.
+#pragma once
+
+#include "block_product.h"
+#include "step_saved.h"
+
+namespace fsdp_block {
+namespace {
+
+// In a forward product n, j and the tiles count the columns of both matrices,
+// n = 2 * inner; in the gradients `inner` columns of the first of dz's two parts
+// lie before column `split`, where the second begins.
+struct PairProduct : Product {
+    const void* b2;
+    int64_t b2_stride, inner, split;
+    // Forward: g and u for the gradient, as values or codes and scales.
+    void *gate, *up;
+    uint8_t *gate_scales, *up_scales;
+    int64_t gate_stride, up_stride, gate_scales_stride, up_scales_stride;
+    // The weights' gradients: the second one.
+    void* out2;
+    int64_t out2_stride;
+};
+
+// Columns of g (or u) in a row of the parts.
+__device__ __host__ __forceinline__ int64_t part_columns(int64_t inner) { return (inner + 7) / 8 * 8; }
+
+// g and u at row i, columns j .. j + 7, of which `left` exist; a quad of lanes has a
+// row's group of 32 columns, and all of it comes here.
+template <typename T>
+__device__ __forceinline__ void keep8(void* kept, uint8_t* scales, int64_t stride, int64_t scales_stride, int64_t i, int64_t j, int left,
+                                      const float (&z)[8]) {
+    if (!kept) return;
+    if (scales)
+        save8(z, left, static_cast<int8_t*>(kept) + i * stride + j, scales + i * scales_stride + j / FSDP_STEP_GROUP);
+    else if (left > 0)
+        store_some(static_cast<T*>(kept) + i * stride + j, left, z);
+}
+template <typename T>
+__device__ __forceinline__ void finish_pair(const PairProduct& p, int64_t i, int64_t j, int left, const float (&g)[8], const float (&u)[8]) {
+    keep8<T>(p.gate, p.gate_scales, p.gate_stride, p.gate_scales_stride, i, j, left, g);
+    keep8<T>(p.up, p.up_scales, p.up_stride, p.up_scales_stride, i, j, left, u);
+    if (left <= 0) return;
+    float out[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) out[c] = act_value<sizeof(T) == 4>(g[c], p.e.act) * u[c];
+    store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, out);
+}
+
+// ------------------------------------------------------------------ forward
+
+// Rows of two matrices: the first half of a tile's from one, the second half from the
+// other.  As Operand, by rows.
+template <typename T, int kRows>
+struct PairRows {
+    using One = Operand<T, kRows, false>;
+    static constexpr int kBytes = One::kBytes, kLoads = One::kLoads, kUnit = One::kUnit;
+    const char* at[2];
+    int64_t left[2];
+    uint32_t offset[kLoads];
+    int k;
+
+    __device__ __forceinline__ PairRows(const PairProduct& p, int64_t first, int64_t k0, int64_t k1) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int u = lane % 8 ^ (wave % 2 * 4 + lane / 16);
+        k = u * kUnit;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t stride = h ? p.b2_stride : p.b_stride;
+            at[h] = static_cast<const char*>(h ? p.b2 : p.b) + (first * stride + k0) * One::kSize;
+            left[h] = (p.inner - 1 - first) * stride * One::kSize + (k1 - k0 + kUnit - 1) / kUnit * 16;
+#pragma unroll
+            for (int j = 0; j < kLoads / 2; ++j) {
+                const int row = (j * 4 + wave) * 8 + lane / 8;
+                offset[h * (kLoads / 2) + j] = uint32_t(min(row * stride * One::kSize + u * 16, One::kNowhere));
+            }
+        }
+    }
+    __device__ __forceinline__ void load(char* lds, int64_t rest) {
+        typedef __attribute__((address_space(3))) void lds_void;
+        constexpr uint32_t kMost = 0x7ffffff0u;
+        const bool mine = k < rest;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t bytes = rest <= 0 ? 0u : uint32_t(min(left[h], int64_t(kMost)));
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at[h]), 0, int(bytes), 0x00020000);
+#pragma unroll
+            for (int j = h * (kLoads / 2); j < (h + 1) * (kLoads / 2); ++j)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + (j * 4 + (threadIdx.x >> 6)) * 1024), 16,
+                                                         int(mine ? offset[j] : uint32_t(One::kNowhere)), 0, 0, 0);
+            at[h] += 128;
+            left[h] -= 128;
+        }
+    }
+};
+
+// out = act(x gate^T) * (x up^T): a wave has the same columns of both products, side
+// by side in its registers and in its piece of LDS.
+struct GatedForward {
+    static constexpr bool kPair = true;
+    template <typename T, int kTileN, bool kColumnsB>
+    using B = PairRows<T, kTileN>;
+    template <typename T, int kTileN, bool kColumnsB>
+    __device__ static __forceinline__ auto operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
+        return B<T, kTileN, kColumnsB>(p, j0 / 2, k0, k1);
+    }
+    // Rows first_i on, columns first_j on of kWide / 2; `pieces` calls back with a piece's
+    // first row and how many it has, once they lie in LDS.
+    template <typename T, int kWide, typename Place, typename Pieces>
+    __device__ static __forceinline__ void finish(const PairProduct& p, int part, const float* turn, Place place, int64_t first_i,
+                                                  int64_t first_j, Pieces pieces) {
+        constexpr int kHalf = kWide / 2, kLanes = kHalf / 8, kStepRows = 64 / kLanes;
+        static_assert(kLanes % 4 == 0);
+        const int lane = threadIdx.x & 63, column = lane % kLanes * 8;
+        const int64_t j = first_j + column;
+        const int left = int(min(p.inner - j, int64_t(8)));
+        pieces([&](int first, int rows) {
+#pragma unroll 1
+            for (int r = lane / kLanes; r < rows; r += kStepRows) {
+                const int64_t i = first_i + first + r;
+                float g[8], u[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    g[c] = turn[place(r, column) + c];
+                    u[c] = turn[place(r, kHalf + column) + c];
+                }
+                if (i >= p.m) continue;
+                if (p.count > 1) {
+                    float* const at = p.parts + (part * p.m + i) * 2 * part_columns(p.inner) + j;
+                    if (left > 0) {
+                        store_some(at, 8, g);
+                        store_some(at + part_columns(p.inner), 8, u);
+                    }
+                } else {
+                    finish_pair<T>(p, i, j, left, g, u);
+                }
+            }
+        });
+    }
+};
+
+// The parts' sums, in order: a thread takes eight columns of g and of u, a quad a
+// group.
+template <typename T>
+__global__ __launch_bounds__(256) void join_gated_kernel(const PairProduct p) {
+    const int64_t wide = part_columns(p.inner), units = (p.inner + 31) / 32 * 4;
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < p.m * units; at += int64_t(gridDim.x) * 256) {
+        const int64_t i = at / units, j = at % units * 8;
+        const int left = int(min(p.inner - j, int64_t(8)));
+        float g[8] = {}, u[8] = {};
+        if (left > 0)
+            for (int s = 0; s < p.count; ++s) {
+                const float* const from = p.parts + (s * p.m + i) * 2 * wide + j;
+                const Eight<float> a = load8(from), b = load8(from + wide);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    g[c] += a[c];
+                    u[c] += b[c];
+                }
+            }
+        finish_pair<T>(p, i, j, left, g, u);
+    }
+}
+
+// ------------------------------------------------------------------ gradients
+
+// dx = [dg | du] [gate_weight; up_weight]: k runs over the first matrix's rows, then
+// from `split` on, a whole number of steps, over the second's.
+template <typename T, int kRows>
+struct JoinedColumns : Operand<T, kRows, true> {
+    using One = Operand<T, kRows, true>;
+    const char* at2;
+    int64_t left2, until;            // bytes of the second matrix; k's before it
+    __device__ __forceinline__ JoinedColumns(const PairProduct& p, int64_t first, int64_t k0, int64_t k1)
+        : One(k0 < p.split ? p.b : p.b2, p.b_stride, first, p.n, k0 < p.split ? k0 : k0 - p.split,
+              min(k0 < p.split ? k1 : k1 - p.split, p.inner)) {
+        at2 = static_cast<const char*>(p.b2) + first * One::kSize;
+        left2 = k1 > p.split ? (min(k1 - p.split, p.inner) - 1) * p.b_stride * One::kSize + (p.n - first + One::kUnit - 1) / One::kUnit * 16 : 0;
+        until = k0 < p.split ? p.split - k0 : INT64_MAX;
+    }
+    __device__ __forceinline__ void load(char* lds, int64_t rest) {
+        if (until <= 0) {
+            this->at = at2;
+            this->left = left2;
+            until = INT64_MAX;
+        }
+        One::load(lds, rest);
+        until -= One::kDeep;
+    }
+};
+
+struct PairInput : OneMatrix {
+    template <typename T, int kTileN, bool kColumnsB>
+    using B = JoinedColumns<T, kTileN>;
+    template <typename T, int kTileN, bool kColumnsB>
+    __device__ static __forceinline__ auto operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
+        return B<T, kTileN, kColumnsB>(p, j0, k0, k1);
+    }
+};
+
+// [dgate_weight; dup_weight] = [dg | du]^T x: rows from `split` on are the second's.
+struct PairWeights : OneMatrix {
+    template <typename T>
+    __device__ static __forceinline__ void store(const PairProduct& p, int64_t i, int64_t j, int left, const float (&z)[8]) {
+        if (i < p.inner) store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
+        else if (i >= p.split) store_some(static_cast<T*>(p.out2) + (i - p.split) * p.out2_stride + j, left, z);
+    }
+};
+
+template <typename T, typename Kind>
+__global__ __launch_bounds__(256) void join_pair_kernel(const PairProduct p) {
+    const int64_t units = (p.n + 7) / 8, stride = units * 8;
+    for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < p.m * units; u += int64_t(gridDim.x) * 256) {
+        const int64_t i = u / units, j = u % units * 8;
+        float z[8] = {};
+        for (int s = 0; s < p.count; ++s) {
+            const Eight<float> v = load8(p.parts + (s * p.m + i) * stride + j);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[c] += v[c];
+        }
+        Kind::template store<T>(p, i, j, int(min(p.n - j, int64_t(8))), z);
+    }
+}
+
+template <typename T, typename Kind, int kTileM, int kTileN, int kSteps>
+__global__ __launch_bounds__(256, (kTilesPerCu<kTileM, kTileN, kSteps>)) void pair_kernel(const PairProduct p) {
+    constexpr bool kForward = std::is_same<Kind, GatedForward>::value, kWeights = std::is_same<Kind, PairWeights>::value;
+    product_tile<T, kWeights, !kForward, kTileM, kTileN, kSteps, Kind>(p);
+}
+
+}  // namespace
+}  // namespace fsdp_block
