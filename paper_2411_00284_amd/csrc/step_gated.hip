@@ -221,12 +221,12 @@ fsdp_status launch_pair(const PairProduct& p, const Form& f, fsdp_dtype dtype, h
                                : launch(pair_kernel<float, Kind, 64, 128, 4>, p, grid, 256, stream);
     const auto of = [&](auto type) {
         using T = decltype(type);
-        if (f.tile_m == 256) return launch(pair_kernel<T, Kind, 256, 256, 2>, p, grid, 256, stream);
+        if (f.tile_m == 256) return launch(ring_kernel<T, Kind, 256, 5>, p, grid, 256, stream);
         if constexpr (kSmallest)
             if (f.tile_n == 64) return launch(pair_kernel<T, Kind, 64, 64, 8>, p, grid, 256, stream);
         if (f.tile_m == 64) return launch(pair_kernel<T, Kind, 64, 128, 4>, p, grid, 256, stream);
-        return f.steps == 2 ? launch(pair_kernel<T, Kind, 128, 128, 2>, p, grid, 256, stream)
-                            : launch(pair_kernel<T, Kind, 128, 128, 4>, p, grid, 256, stream);
+        return f.steps == 2 ? launch(ring_kernel<T, Kind, 128, 5>, p, grid, 256, stream)
+                            : launch(ring_kernel<T, Kind, 128, 10>, p, grid, 256, stream);
     };
     return dtype == FSDP_DTYPE_BF16 ? of(bf16(0.f)) : of(f16(0.f));
 }

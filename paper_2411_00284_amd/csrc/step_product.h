@@ -5,6 +5,7 @@
 
 #include "block_product.h"
 #include "step_saved.h"
+#include "step_tile.h"
 
 namespace fsdp_block {
 namespace {
@@ -96,6 +97,36 @@ struct PairRows {
     }
 };
 
+// The same for step_tile.h.
+template <typename T, int kRows>
+struct PairStream : Stream<T, kRows, false> {
+    using One = Stream<T, kRows, false>;
+    static constexpr int kHalf = One::kLoads / 2;
+    const char* at2;
+    int64_t left2;
+    __amdgpu_buffer_rsrc_t from2;
+    __device__ __forceinline__ PairStream(const PairProduct& p, int64_t first, int64_t k0, int64_t k1)
+        : One(p.b, p.b_stride, first, p.inner, k0, k1) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        at2 = static_cast<const char*>(p.b2) + (first * p.b2_stride + k0) * 2;
+        left2 = (p.inner - 1 - first) * p.b2_stride * 2 + (k1 - k0 + 7) / 8 * 16;
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j)
+            this->offset[kHalf + j] = uint32_t(min(((j * 4 + wave) * 8 + lane / 8) * p.b2_stride * 2 + this->k * 2, One::kNowhere));
+    }
+    __device__ __forceinline__ void next() {
+        from2 = this->range(at2, left2);
+        at2 += 128;
+        left2 -= 128;
+        One::next();
+    }
+    __device__ __forceinline__ void load(char* lds, int j, int wave) const {
+        typedef __attribute__((address_space(3))) void lds_void;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kHalf ? this->from : from2, (lds_void*)(lds + (j * 4 + wave) * 1024), 16,
+                                                 int(this->offset[j]), 0, 0, 0);
+    }
+};
+
 // out = act(x gate^T) * (x up^T): a wave has the same columns of both products, side
 // by side in its registers and in its piece of LDS.
 struct GatedForward {
@@ -105,6 +136,12 @@ struct GatedForward {
     template <typename T, int kTileN, bool kColumnsB>
     __device__ static __forceinline__ auto operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
         return B<T, kTileN, kColumnsB>(p, j0 / 2, k0, k1);
+    }
+    template <typename T, int kTile, bool kColumnsB>
+    using Ring = PairStream<T, kTile>;
+    template <typename T, int kTile, bool kColumnsB>
+    __device__ static __forceinline__ auto ring_operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
+        return PairStream<T, kTile>(p, j0 / 2, k0, k1);
     }
     // Rows first_i on, columns first_j on of kWide / 2; `pieces` calls back with a piece's
     // first row and how many it has, once they lie in LDS.
@@ -191,17 +228,79 @@ struct JoinedColumns : Operand<T, kRows, true> {
     }
 };
 
-struct PairInput : OneMatrix {
+// The same for step_tile.h.
+template <typename T, int kRows>
+struct JoinedStream : Stream<T, kRows, true> {
+    using One = Stream<T, kRows, true>;
+    const char* at2;
+    int64_t left2, until;
+    __device__ __forceinline__ JoinedStream(const PairProduct& p, int64_t first, int64_t k0, int64_t k1)
+        : One(k0 < p.split ? p.b : p.b2, p.b_stride, first, p.n, k0 < p.split ? k0 : k0 - p.split,
+              min(k0 < p.split ? k1 : k1 - p.split, p.inner)) {
+        at2 = static_cast<const char*>(p.b2) + first * 2;
+        left2 = k1 > p.split ? (min(k1 - p.split, p.inner) - 1) * p.b_stride * 2 + (p.n - first + 7) / 8 * 16 : 0;
+        until = k0 < p.split ? p.split - k0 : INT64_MAX;
+        this->rest = k1 - k0;
+    }
+    __device__ __forceinline__ void next() {
+        if (until <= 0) {
+            this->at = at2;
+            this->left = left2;
+            until = INT64_MAX;
+        }
+        One::next();
+        until -= 64;
+    }
+};
+
+// eight columns of a row to their place.
+template <typename Kind>
+struct Plain : OneMatrix {
+    template <typename T, int kWide, typename Place, typename Pieces>
+    __device__ static __forceinline__ void finish(const PairProduct& p, int part, const float* turn, Place place, int64_t first_i,
+                                                  int64_t first_j, Pieces pieces) {
+        constexpr int kLanes = kWide / 8, kStepRows = 64 / kLanes;
+        const int lane = threadIdx.x & 63, column = lane % kLanes * 8;
+        const int64_t j = first_j + column;
+        const int left = int(min(p.n - j, int64_t(8)));
+        pieces([&](int first, int rows) {
+#pragma unroll 4
+            for (int r = lane / kLanes; r < rows; r += kStepRows) {
+                const int64_t i = first_i + first + r;
+                float z[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) z[c] = turn[place(r, column) + c];
+                if (i >= p.m || left <= 0) continue;
+                if (p.count > 1) store_some(p.parts + (part * p.m + i) * ((p.n + 7) / 8 * 8) + j, 8, z);
+                else Kind::template store<T>(p, i, j, left, z);
+            }
+        });
+    }
+};
+
+struct PairInput : Plain<PairInput> {
     template <typename T, int kTileN, bool kColumnsB>
     using B = JoinedColumns<T, kTileN>;
     template <typename T, int kTileN, bool kColumnsB>
     __device__ static __forceinline__ auto operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
         return B<T, kTileN, kColumnsB>(p, j0, k0, k1);
     }
+    template <typename T, int kTile, bool kColumnsB>
+    using Ring = JoinedStream<T, kTile>;
+    template <typename T, int kTile, bool kColumnsB>
+    __device__ static __forceinline__ auto ring_operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
+        return JoinedStream<T, kTile>(p, j0, k0, k1);
+    }
 };
 
 // [dgate_weight; dup_weight] = [dg | du]^T x: rows from `split` on are the second's.
-struct PairWeights : OneMatrix {
+struct PairWeights : Plain<PairWeights> {
+    template <typename T, int kTile, bool kColumnsB>
+    using Ring = Stream<T, kTile, true>;
+    template <typename T, int kTile, bool kColumnsB>
+    __device__ static __forceinline__ auto ring_operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
+        return Stream<T, kTile, true>(p.b, p.b_stride, j0, p.n, k0, k1);
+    }
     template <typename T>
     __device__ static __forceinline__ void store(const PairProduct& p, int64_t i, int64_t j, int left, const float (&z)[8]) {
         if (i < p.inner) store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, z);
@@ -228,6 +327,13 @@ template <typename T, typename Kind, int kTileM, int kTileN, int kSteps>
 __global__ __launch_bounds__(256, (kTilesPerCu<kTileM, kTileN, kSteps>)) void pair_kernel(const PairProduct p) {
     constexpr bool kForward = std::is_same<Kind, GatedForward>::value, kWeights = std::is_same<Kind, PairWeights>::value;
     product_tile<T, kWeights, !kForward, kTileM, kTileN, kSteps, Kind>(p);
+}
+
+// Tiles of step_tile.h; with kRing = 5 of 128 x 128 two lie on a CU.
+template <typename T, typename Kind, int kTile, int kRing>
+__global__ __launch_bounds__(256, (kTile * kRing > 640 ? 1 : 2)) void ring_kernel(const PairProduct p) {
+    constexpr bool kForward = std::is_same<Kind, GatedForward>::value, kWeights = std::is_same<Kind, PairWeights>::value;
+    ring_tile<T, kWeights, !kForward, kTile, kRing, Kind>(p);
 }
 
 }  // namespace
