@@ -120,9 +120,9 @@ struct PairStream : Stream<T, kRows, false> {
         left2 -= 128;
         One::next();
     }
-    __device__ __forceinline__ void load(char* lds, int j, int wave) const {
+    __device__ __forceinline__ void load(char* lds, int j, int own) const {
         typedef __attribute__((address_space(3))) void lds_void;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kHalf ? this->from : from2, (lds_void*)(lds + (j * 4 + wave) * 1024), 16,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(j < kHalf ? this->from : from2, (lds_void*)(lds + j * 4096 + own), 16,
                                                  int(this->offset[j]), 0, 0, 0);
     }
 };
@@ -233,20 +233,21 @@ template <typename T, int kRows>
 struct JoinedStream : Stream<T, kRows, true> {
     using One = Stream<T, kRows, true>;
     const char* at2;
-    int64_t left2, until;
+    int64_t left2;
+    int until;
     __device__ __forceinline__ JoinedStream(const PairProduct& p, int64_t first, int64_t k0, int64_t k1)
         : One(k0 < p.split ? p.b : p.b2, p.b_stride, first, p.n, k0 < p.split ? k0 : k0 - p.split,
               min(k0 < p.split ? k1 : k1 - p.split, p.inner)) {
         at2 = static_cast<const char*>(p.b2) + first * 2;
         left2 = k1 > p.split ? (min(k1 - p.split, p.inner) - 1) * p.b_stride * 2 + (p.n - first + 7) / 8 * 16 : 0;
-        until = k0 < p.split ? p.split - k0 : INT64_MAX;
-        this->rest = k1 - k0;
+        until = k0 < p.split ? int(min(p.split - k0, int64_t(INT32_MAX))) : INT32_MAX;
+        this->rest = int(k1 - k0);
     }
     __device__ __forceinline__ void next() {
         if (until <= 0) {
             this->at = at2;
             this->left = left2;
-            until = INT64_MAX;
+            until = INT32_MAX;
         }
         One::next();
         until -= 64;

@@ -64,7 +64,7 @@ struct Stream {
 
     const char* at;            // the next step's first byte
     int64_t step, left;        // bytes to the step after it, and to the operand's end, in whole units
-    int64_t rest;              // k not yet asked for
+    int rest;                  // k not yet asked for
     uint32_t offset[kLoads];
     int k;                     // this lane's first k of a step ("rows")
     __amdgpu_buffer_rsrc_t from;
@@ -83,7 +83,7 @@ struct Stream {
     __device__ __forceinline__ Stream(const void* p, int64_t stride, int64_t first, int64_t rows, int64_t k0, int64_t k1) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         begin_at(p, stride, first, rows, k0, k1);
-        rest = k1 - k0;
+        rest = int(k1 - k0);
         k = (lane % 8 ^ (wave % 2 * 4 + lane / 16)) * 8;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
@@ -95,8 +95,10 @@ struct Stream {
             }
         }
     }
+    // (`bytes` is not negative while there is something to ask for; what passes 31 bits is out of any tile's reach.)
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t range(const char* p, int64_t bytes) const {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, int(rest <= 0 ? 0u : uint32_t(min(bytes, int64_t(kMost)))), 0x00020000);
+        const uint32_t n = uint64_t(bytes) >> 31 ? kMost : uint32_t(bytes);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, int(rest <= 0 ? 0u : n), 0x00020000);
     }
     // Units of the last step that lie past k are asked for out of range, and so are zeros.
     __device__ __forceinline__ void cut() {
@@ -112,9 +114,10 @@ struct Stream {
         left -= step;
         rest -= 64;
     }
-    __device__ __forceinline__ void load(char* lds, int j, int wave) const {
+    // `own`: 1024 times the wave.
+    __device__ __forceinline__ void load(char* lds, int j, int own) const {
         typedef __attribute__((address_space(3))) void lds_void;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + (j * 4 + wave) * 1024), 16, int(offset[j]), 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + j * 4096 + own), 16, int(offset[j]), 0, 0, 0);
     }
 };
 
@@ -137,17 +140,20 @@ struct Half {
             }
         }
     }
-    __device__ __forceinline__ void read(const char* lds, const int (&place)[kPlaces], int half, int x) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    static constexpr int kReads = kColumns ? 2 * kTiles : kTiles;      // LDS instructions
+    s16x4 low;                       // the first of two
+    // Read `i` of kReads, in order.
+    __device__ __forceinline__ void read(const char* lds, const int (&place)[kPlaces], int half, int i) {
         if constexpr (!kColumns) {
-            v[x] = *reinterpret_cast<const Eight<T>*>(lds + place[half] + (x * 16 + (x >= kTiles / 2 ? kApart : 0)) * 128);
+            v[i] = *reinterpret_cast<const Eight<T>*>(lds + place[half] + (i * 16 + (i >= kTiles / 2 ? kApart : 0)) * 128);
         } else {
             // The transposing load gives lane i of 16 the i-th column of their block.
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const char* const at = lds + place[x] + half * 32 * kRows * 2;
-            v[x] = __builtin_bit_cast(Eight<T>, __builtin_shufflevector(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at),
-                                                                       __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * kRows * 2)),
-                                                                       0, 1, 2, 3, 4, 5, 6, 7));
+            const int x = i / 2;
+            const s16x4 got = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + place[x] + half * 32 * kRows * 2 + i % 2 * 4 * kRows * 2));
+            if (i % 2 == 0) low = got;
+            else v[x] = __builtin_bit_cast(Eight<T>, __builtin_shufflevector(low, got, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     }
 };
@@ -196,10 +202,10 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
         __builtin_amdgcn_sched_barrier(0);
     };
     // The q-th operand of all (A of step q / 2 for even q, else B) to its place.
-    const auto ask = [&](auto q, int j) {
+    const auto ask = [&](auto q, int j, int own) {
         constexpr int kQ = decltype(q)::value;
-        if constexpr (kQ % 2 == 0) a.load(ring[kQ % kRing], j, wave);
-        else b.load(ring[kQ % kRing], j, wave);
+        if constexpr (kQ % 2 == 0) a.load(ring[kQ % kRing], j, own);
+        else b.load(ring[kQ % kRing], j, own);
     };
     const auto next = [&](auto q) {
         if constexpr (decltype(q)::value % 2 == 0) a.next();
@@ -208,18 +214,29 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     // The matrix instructions of the half in registers `kS`, the reads of the other half (half
     // kS ^ 1 of the step whose A is the kQ-th operand), the loads of operand kAsk; in this order.
     const auto half = [&](auto s, auto q, auto asked) {
-        constexpr int kS = decltype(s)::value, kQ = decltype(q)::value, kEvery = kN * kN / 2 / kLoads;
+        constexpr int kS = decltype(s)::value, kQ = decltype(q)::value, kAll = kN * kN;
+        // Both operands' reads, one after each of the first half of the matrix instructions (or each
+        // second one of them, if there are as few); the loads between them, or after them.
+        constexpr int kReads = FA::kReads + FB::kReads, kGap = kReads * 4 <= kAll ? 2 : 1;
+        constexpr bool kBetween = kGap == 2;
+        constexpr int kFirst = kBetween ? 1 : kAll / 2, kEvery = kAll / 2 / kLoads;
+        int own = wave * 1024;
+        asm volatile("" : "+s"(own));            // an addition a load, instead of a register for each place and load
 #pragma unroll
-        for (int i = 0; i < kN * kN; ++i) {
-            if (i % 2 == 0 && i / 2 < 2 * kN) {
+        for (int i = 0; i < kAll; ++i) {
+            if (i % kGap == 0 && i / kGap < kReads) {
+                constexpr int kFew = FA::kReads < FB::kReads ? FA::kReads : FB::kReads;
+                // In turn, as long as there are two.
+                const int r = i / kGap, a_reads = r < 2 * kFew ? (r + 1) / 2 : FA::kReads > kFew ? r - kFew : kFew;
+                const bool from_a = r < 2 * kFew ? r % 2 == 0 : FA::kReads > kFew;
                 __builtin_amdgcn_sched_barrier(0);
-                if (i / 2 % 2 == 0) fa[kS ^ 1].read(ring[kQ % kRing], pa, kS ^ 1, i / 4);
-                else fb[kS ^ 1].read(ring[(kQ + 1) % kRing], pb, kS ^ 1, i / 4);
+                if (from_a) fa[kS ^ 1].read(ring[kQ % kRing], pa, kS ^ 1, a_reads);
+                else fb[kS ^ 1].read(ring[(kQ + 1) % kRing], pb, kS ^ 1, r - a_reads);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (i % kEvery == 1 && i / kEvery < kLoads) {
+            if (i >= kFirst && (i - kFirst) % kEvery == 0 && (i - kFirst) / kEvery < kLoads) {
                 __builtin_amdgcn_sched_barrier(0);
-                ask(asked, i / kEvery);
+                ask(asked, (i - kFirst) / kEvery, own);
                 __builtin_amdgcn_sched_barrier(0);
             }
             mma16(fa[kS].v[i / kN], fb[kS].v[i % kN], acc[i / kN][i % kN]);
@@ -240,7 +257,7 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     const auto start = [&](auto q) {
         next(q);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) ask(q, j);
+        for (int j = 0; j < kLoads; ++j) ask(q, j, wave * 1024);
     };
     start(std::integral_constant<int, 0>());
     start(std::integral_constant<int, 1>());
@@ -255,12 +272,11 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     }
     sync(std::integral_constant<int, kRing - 3>());
 #pragma unroll
-    for (int x = 0; x < kN; ++x) {
-        fa[0].read(r0, pa, 0, x);
-        fb[0].read(r1, pb, 0, x);
-    }
+    for (int r = 0; r < FA::kReads; ++r) fa[0].read(r0, pa, 0, r);
+#pragma unroll
+    for (int r = 0; r < FB::kReads; ++r) fb[0].read(r1, pb, 0, r);
     // Steps past the end add zeros: the loop takes a period at a time.
-    for (int64_t left = k1 - k0; left > 0; left -= 64 * kPeriod) {
+    for (int left = int(k1 - k0); left > 0; left -= 64 * kPeriod) {
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());
         step(std::integral_constant<int, 2>());
