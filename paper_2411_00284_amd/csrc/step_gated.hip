@@ -135,15 +135,17 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(const GatedSlopeArgs a
             d.load(a.dout, nullptr, a.dout_stride, 0, i, j, left);
             g.load(a.gate, a.gate_scales, a.gate_stride, a.gate_scales_stride, i, j, left);
             u.load(a.up, a.up_scales, a.up_stride, a.up_scales_stride, i, j, left);
+            with_act(a.act, [&](auto act) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                float value, slope;
-                act_both<sizeof(T) == 4>(g[c], a.act, value, slope);
-                out[c] = value * u[c];
-                const bool held = c < left;              // past the row's end the values stand for nothing
-                dg[c] = held ? d[c] * u[c] * slope : 0.f;
-                du[c] = held ? d[c] * value : 0.f;
-            }
+                for (int c = 0; c < 8; ++c) {
+                    float value, slope;
+                    act_both<sizeof(T) == 4>(g[c], decltype(act)::value, value, slope);
+                    out[c] = value * u[c];
+                    const bool held = c < left;          // past the row's end the values stand for nothing
+                    dg[c] = held ? d[c] * u[c] * slope : 0.f;
+                    du[c] = held ? d[c] * value : 0.f;
+                }
+            });
             if (a.out) store_some(static_cast<T*>(a.out) + i * a.out_stride + j, left, out);
         }
         if (a.dz) {
@@ -183,16 +185,18 @@ __global__ __launch_bounds__(256) void saved_slope_kernel(const SavedSlopeArgs a
                 d.load(a.dout, nullptr, a.dout_stride, 0, i, j, left);
                 if (a.pre) z.load(a.pre, a.pre_scales, a.pre_stride, a.pre_scales_stride, i, j, left);
                 if (a.times) f.load(a.times, nullptr, a.times_stride, 0, i, j, left);
+                with_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    float value = 1.f, slope = 1.f, v = d[c];
-                    if (a.pre) act_both<sizeof(T) == 4>(z[c], a.act, value, slope);
-                    df[c] = v * value;
-                    if (a.times) v *= f[c];
-                    if (a.act != FSDP_ACT_NONE) v *= slope;
-                    dz[c] = c < left ? v : 0.f;
-                    sum[c] += dz[c];
-                }
+                    for (int c = 0; c < 8; ++c) {
+                        float value = 1.f, slope = 1.f, v = d[c];
+                        if (a.pre) act_both<sizeof(T) == 4>(z[c], decltype(act)::value, value, slope);
+                        df[c] = v * value;
+                        if (a.times) v *= f[c];
+                        if (decltype(act)::value != FSDP_ACT_NONE) v *= slope;
+                        dz[c] = c < left ? v : 0.f;
+                        sum[c] += dz[c];
+                    }
+                });
                 if (a.dtimes) store_some(static_cast<T*>(a.dtimes) + i * a.dtimes_stride + j, left, df);
             }
             if (a.dz) store_some(static_cast<T*>(a.dz) + i * a.dz_stride + j, 8, dz);

@@ -28,25 +28,40 @@ struct PairProduct : Product {
 // Columns of g (or u) in a row of the parts.
 __device__ __host__ __forceinline__ int64_t part_columns(int64_t inner) { return (inner + 7) / 8 * 8; }
 
-// g and u at row i, columns j .. j + 7, of which `left` exist; a quad of lanes has a
-// row's group of 32 columns, and all of it comes here.
-template <typename T>
+// f(activation) with the activation as a constant: one choice for many values, so that
+// their chains of instructions overlap.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case FSDP_ACT_RELU: return f(std::integral_constant<int, FSDP_ACT_RELU>());
+        case FSDP_ACT_SILU: return f(std::integral_constant<int, FSDP_ACT_SILU>());
+        case FSDP_ACT_GELU: return f(std::integral_constant<int, FSDP_ACT_GELU>());
+        case FSDP_ACT_GELU_TANH: return f(std::integral_constant<int, FSDP_ACT_GELU_TANH>());
+        default: return f(std::integral_constant<int, FSDP_ACT_NONE>());
+    }
+}
+
+// g and u at row i, columns j .. j + 7, of which `left` exist; four lanes (kApart: as in
+// group_max) have a row's group of 32 columns, and all of them come here.
+template <typename T, bool kApart>
 __device__ __forceinline__ void keep8(void* kept, uint8_t* scales, int64_t stride, int64_t scales_stride, int64_t i, int64_t j, int left,
                                       const float (&z)[8]) {
     if (!kept) return;
     if (scales)
-        save8(z, left, static_cast<int8_t*>(kept) + i * stride + j, scales + i * scales_stride + j / FSDP_STEP_GROUP);
+        save8<kApart>(z, left, static_cast<int8_t*>(kept) + i * stride + j, scales + i * scales_stride + j / FSDP_STEP_GROUP);
     else if (left > 0)
         store_some(static_cast<T*>(kept) + i * stride + j, left, z);
 }
-template <typename T>
+template <typename T, bool kApart = false>
 __device__ __forceinline__ void finish_pair(const PairProduct& p, int64_t i, int64_t j, int left, const float (&g)[8], const float (&u)[8]) {
-    keep8<T>(p.gate, p.gate_scales, p.gate_stride, p.gate_scales_stride, i, j, left, g);
-    keep8<T>(p.up, p.up_scales, p.up_stride, p.up_scales_stride, i, j, left, u);
+    keep8<T, kApart>(p.gate, p.gate_scales, p.gate_stride, p.gate_scales_stride, i, j, left, g);
+    keep8<T, kApart>(p.up, p.up_scales, p.up_stride, p.up_scales_stride, i, j, left, u);
     if (left <= 0) return;
     float out[8];
+    with_act(p.e.act, [&](auto act) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) out[c] = act_value<sizeof(T) == 4>(g[c], p.e.act) * u[c];
+        for (int c = 0; c < 8; ++c) out[c] = act_value<sizeof(T) == 4>(g[c], decltype(act)::value) * u[c];
+    });
     store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, out);
 }
 
@@ -108,11 +123,14 @@ struct PairStream : Stream<T, kRows, false> {
     __device__ __forceinline__ PairStream(const PairProduct& p, int64_t first, int64_t k0, int64_t k1)
         : One(p.b, p.b_stride, first, p.inner, k0, k1) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        this->k = (lane % 8 ^ (wave * 2 + lane / 16 % 2)) * 8;       // as a woven Half reads them
         at2 = static_cast<const char*>(p.b2) + (first * p.b2_stride + k0) * 2;
         left2 = (p.inner - 1 - first) * p.b2_stride * 2 + (k1 - k0 + 7) / 8 * 16;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j)
+        for (int j = 0; j < kHalf; ++j) {
+            this->offset[j] = uint32_t(min(((j * 4 + wave) * 8 + lane / 8) * p.b_stride * 2 + this->k * 2, One::kNowhere));
             this->offset[kHalf + j] = uint32_t(min(((j * 4 + wave) * 8 + lane / 8) * p.b2_stride * 2 + this->k * 2, One::kNowhere));
+        }
     }
     __device__ __forceinline__ void next() {
         from2 = this->range(at2, left2);
@@ -143,6 +161,24 @@ struct GatedForward {
     __device__ static __forceinline__ auto ring_operand(const PairProduct& p, int64_t j0, int64_t k0, int64_t k1) {
         return PairStream<T, kTile>(p, j0 / 2, k0, k1);
     }
+    // Eight columns of a row from a ring tile's registers: lanes 16 apart have a group of 32.
+    template <typename T>
+    __device__ static __forceinline__ void put(const PairProduct& p, int part, int64_t i, int64_t j, const float (&g)[8], const float (&u)[8]) {
+        const int left = int(min(p.inner - j, int64_t(8)));
+        if (i >= p.m) return;
+        if (p.count > 1) {
+            store_parts(p, part, i, j, left, g, u);
+        } else {
+            finish_pair<T, true>(p, i, j, left, g, u);
+        }
+    }
+    __device__ static __forceinline__ void store_parts(const PairProduct& p, int part, int64_t i, int64_t j, int left, const float (&g)[8],
+                                                       const float (&u)[8]) {
+        float* const at = p.parts + (part * p.m + i) * 2 * part_columns(p.inner) + j;
+        if (left <= 0) return;
+        store_some(at, 8, g);
+        store_some(at + part_columns(p.inner), 8, u);
+    }
     // Rows first_i on, columns first_j on of kWide / 2; `pieces` calls back with a piece's
     // first row and how many it has, once they lie in LDS.
     template <typename T, int kWide, typename Place, typename Pieces>
@@ -164,15 +200,8 @@ struct GatedForward {
                     u[c] = turn[place(r, kHalf + column) + c];
                 }
                 if (i >= p.m) continue;
-                if (p.count > 1) {
-                    float* const at = p.parts + (part * p.m + i) * 2 * part_columns(p.inner) + j;
-                    if (left > 0) {
-                        store_some(at, 8, g);
-                        store_some(at + part_columns(p.inner), 8, u);
-                    }
-                } else {
-                    finish_pair<T>(p, i, j, left, g, u);
-                }
+                if (p.count > 1) store_parts(p, part, i, j, left, g, u);
+                else finish_pair<T>(p, i, j, left, g, u);
             }
         });
     }

@@ -35,20 +35,28 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
     return byte == kNotFinite ? NAN : __builtin_bit_cast(float, byte ? byte << 23 : 0x400000u);
 }
 
-// The largest over the four lanes of a quad.
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+// The largest over the four lanes that hold a group: a quad, or (kApart) lanes 16 apart.
+template <bool kApart>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+    if constexpr (kApart) {
+        const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);     // rows of 16 lanes: 0 1 2 3 -> 0 0 2 2, 1 1 3 3
+        v = max(a[0], a[1]);
+        const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);     // halves: 0 1 -> 0 0, 1 1
+        return max(b[0], b[1]);
+    }
     v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xf, 0xf, false)));      // lanes 1 0 3 2
     return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xf, 0xf, false)));   // lanes 2 3 0 1
 }
 
-// A lane's eight columns of a group, whose other columns its quad holds: all four
-// lanes are active and call it, those past the row's end with left <= 0.
+// A lane's eight columns of a group, whose other columns three more lanes hold (group_max): all
+// four are active and call it, those past the row's end with left <= 0.
+template <bool kApart = false>
 __device__ __forceinline__ void save8(const float (&v)[8], int left, int8_t* codes, uint8_t* scale) {
     uint32_t most = 0;
 #pragma unroll
     for (int c = 0; c < 8; ++c)
         if (c < left) most = max(most, __builtin_bit_cast(uint32_t, v[c]) & 0x7fffffffu);
-    const uint32_t byte = scale_byte(quad_max(most));
+    const uint32_t byte = scale_byte(group_max<kApart>(most));
     if (left <= 0) return;
     // A factor of 0 makes an infinity a NaN, whose code is no matter: it is 0.
     const float inverse = scale_inverse(byte == kNotFinite ? 1u : byte);
@@ -62,7 +70,7 @@ __device__ __forceinline__ void save8(const float (&v)[8], int left, int8_t* cod
         for (int c = 0; c < 8; ++c)
             if (c < left) codes[c] = q[c];
     }
-    if ((threadIdx.x & 3) == 0) *scale = uint8_t(byte);
+    if ((threadIdx.x & (kApart ? 48 : 3)) == 0) *scale = uint8_t(byte);
 }
 
 // Eight values of one group, zeros after the first n.

@@ -123,7 +123,9 @@ struct Stream {
 
 // A wave's registers of half a step: kTiles times 16 rows of an operand. kApart: how many
 // rows lie between the first half of the tiles and the second, over what they cover.
-template <typename T, int kRows, bool kColumns, int kTiles, int kApart>
+// kWoven ("rows"): tiles 2 y and 2 y + 1 have 32 rows in turns of four, tile 2 y the first four of
+// each eight; LDS then exchanges the units of row r by (r / 8 % 4) * 2 + r / 2 % 2.
+template <typename T, int kRows, bool kColumns, int kTiles, int kApart, bool kWoven = false>
 struct Half {
     static constexpr int kPlaces = kColumns ? kTiles : 2;
     Eight<T> v[kTiles];
@@ -131,7 +133,9 @@ struct Half {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int x = 0; x < kPlaces; ++x) {
-            if constexpr (!kColumns) {
+            if constexpr (kWoven) {
+                place[x] = (first + lane % 16 / 4 * 8 + lane % 4) * 128 + ((4 * x + lane / 16) ^ (lane % 16 / 4 * 2 + lane % 4 / 2)) * 16;
+            } else if constexpr (!kColumns) {
                 place[x] = (first + lane % 16) * 128 + ((4 * x + lane / 16) ^ lane / 2 % 8) * 16;
             } else {
                 // The 4 x 16 block of k and columns that 16 lanes point to; k + 4 and k + 32 are exchanged alike.
@@ -147,7 +151,8 @@ struct Half {
     // Read `i` of kReads, in order.
     __device__ __forceinline__ void read(const char* lds, const int (&place)[kPlaces], int half, int i) {
         if constexpr (!kColumns) {
-            v[i] = *reinterpret_cast<const Eight<T>*>(lds + place[half] + (i * 16 + (i >= kTiles / 2 ? kApart : 0)) * 128);
+            const int row = (kWoven ? i / 2 * 32 + i % 2 * 4 : i * 16) + (i >= kTiles / 2 ? kApart : 0);
+            v[i] = *reinterpret_cast<const Eight<T>*>(lds + place[half] + row * 128);
         } else {
             // The transposing load gives lane i of 16 the i-th column of their block.
             const int x = i / 2;
@@ -178,7 +183,7 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     A a(p.a, p.a_stride, i0, p.m, k0, k1);
     B b = Kind::template ring_operand<T, kTile, kColumnsB>(p, j0, k0, k1);
     using FA = Half<T, kTile, kColumnsA, kN, 0>;
-    using FB = Half<T, kTile, kColumnsB, kN, Kind::kPair ? kTile / 4 : 0>;
+    using FB = Half<T, kTile, kColumnsB, kN, Kind::kPair ? kTile / 4 : 0, Kind::kPair>;
     FA fa[2];
     FB fb[2];
     int pa[FA::kPlaces], pb[FB::kPlaces];
@@ -239,7 +244,10 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
                 ask(asked, (i - kFirst) / kEvery, own);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            mma16(fa[kS].v[i / kN], fb[kS].v[i % kN], acc[i / kN][i % kN]);
+            // A pair's sums lie the other way round: a lane has a row of A and, of two woven tiles of B, eight
+            // neighbouring columns.
+            if constexpr (Kind::kPair) mma16(fb[kS].v[i % kN], fa[kS].v[i / kN], acc[i / kN][i % kN]);
+            else mma16(fa[kS].v[i / kN], fb[kS].v[i % kN], acc[i / kN][i % kN]);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -287,6 +295,33 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     settle(acc);
     sync(std::integral_constant<int, 0>());                       // nothing more is written to LDS
 
+    if constexpr (Kind::kPair) {
+        // A lane finishes what it holds, a row's 64 bytes of four lanes at a time. It passes the sums through
+        // LDS all the same, its own only: so that the code of eight columns is there once.
+        typedef float Acc4x64[64][4];
+        static_assert(4 * kN * sizeof(Acc4x64) <= kBytes);
+        Acc4x64* const mine = reinterpret_cast<Acc4x64*>(wave == 0 ? r0 : wave == 1 ? r1 : wave == 2 ? r2 : r3);
+        const int64_t j = (j0 + wj) / 2 + lane / 16 * 8;
+#pragma unroll
+        for (int x0 = 0; x0 < kN; x0 += 4) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int y = 0; y < kN; ++y) *reinterpret_cast<Acc4*>(mine[x * kN + y][lane]) = acc[x0 + x][y];
+#pragma unroll 1
+            for (int at = 0; at < kN; ++at) {
+                const int x = at / (kN / 4), y = at % (kN / 4) * 2;
+                float g[8], u[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    g[c] = mine[x * kN + y + c / 4][lane][c % 4];
+                    u[c] = mine[x * kN + kN / 2 + y + c / 4][lane][c % 4];
+                }
+                Kind::template put<T>(p, t.part, i0 + wi + 16 * (x0 + x) + lane % 16, j + 16 * y, g, u);
+            }
+        }
+        return;
+    } else {
     // A wave passes its sums through a place of the ring of its own, 64 rows at a time, so
     // that a lane gets eight neighbouring columns; no barrier of the workgroup is needed, the
     // fences keep the lanes' writes before other lanes' reads, and those before the next writes.
@@ -294,7 +329,7 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
     static_assert(kTurnRows * kWide * 4 <= kBytes && kWide % kTurnRows == 0);
     float* const turn = reinterpret_cast<float*>(wave == 0 ? r0 : wave == 1 ? r1 : wave == 2 ? r2 : r3);
     const auto place = [](int row, int column) { return row * kWide + (column ^ row / 4 % 4 * 16); };
-    Kind::template finish<T, kWide>(p, t.part, turn, place, i0 + wi, Kind::kPair ? (j0 + wj) / 2 : j0 + wj, [&](auto each) {
+    Kind::template finish<T, kWide>(p, t.part, turn, place, i0 + wi, j0 + wj, [&](auto each) {
 #pragma unroll
         for (int x0 = 0; x0 < kN; x0 += 4) {
 #pragma unroll
@@ -310,6 +345,7 @@ __device__ __forceinline__ void ring_tile(const Args& p) {
             __builtin_amdgcn_wave_barrier();
         }
     });
+    }
 }
 
 }  // namespace
