@@ -18,19 +18,50 @@ struct SaveArgs {
     int64_t x_stride, codes_stride, scales_stride, cols, runs, items;
 };
 
+// Items of a wave: kTogether neighbouring ones, all asked for before the first is worked on.
+// Each is a place in the matrix: this lane's eight columns.
+constexpr int kTogether = 4;
+struct Place {
+    int64_t row, j;
+    int left;                        // columns from j on; 0 and less: none
+};
+template <typename F>
+__device__ __forceinline__ void for_items(int64_t items, int64_t runs, int64_t cols, F f) {
+    for (int64_t first = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * kTogether; first < items; first += int64_t(gridDim.x) * 4 * kTogether) {
+        Place at[kTogether];
+        int64_t row = first / runs, run = first - row * runs;
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            at[u] = {row, (run * 64 + threadIdx.x % 64) * 8, 0};
+            at[u].left = first + u < items ? int(min(cols - at[u].j, int64_t(8))) : -1;
+            if (++run == runs) {
+                run = 0;
+                ++row;
+            }
+        }
+        f(at);
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void save_kernel(const SaveArgs a) {
-    for (int64_t item = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; item < a.items; item += int64_t(gridDim.x) * 4) {
-        const int64_t row = item / a.runs, j = ((item - row * a.runs) * 64 + threadIdx.x % 64) * 8;
-        const int left = int(min(a.cols - j, int64_t(8)));
-        float v[8] = {};
-        if (left > 0) {
-            const Eight<T> in = load_some(static_cast<const T*>(a.x) + row * a.x_stride + j, left);
+    for_items(a.items, a.runs, a.cols, [&](const Place (&at)[kTogether]) {
+        Eight<T> in[kTogether];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = float(in[c]);
+        for (int u = 0; u < kTogether; ++u) {
+            const T* const x = static_cast<const T*>(a.x) + at[u].row * a.x_stride + at[u].j;
+            if (at[u].left >= 8) in[u] = load8_once(x);
+            else in[u] = load_some(x, at[u].left);
         }
-        save8(v, left, a.codes + row * a.codes_stride + j, a.scales + row * a.scales_stride + j / FSDP_STEP_GROUP);
-    }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = float(in[u][c]);
+            save8(v, at[u].left, a.codes + at[u].row * a.codes_stride + at[u].j,
+                  a.scales + at[u].row * a.scales_stride + at[u].j / FSDP_STEP_GROUP);
+        }
+    });
 }
 
 struct RestoreArgs {
@@ -43,19 +74,25 @@ struct RestoreArgs {
 // Columns cols .. to_cols - 1 become zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void restore_kernel(const RestoreArgs a) {
-    for (int64_t item = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; item < a.items; item += int64_t(gridDim.x) * 4) {
-        const int64_t row = item / a.runs, j = ((item - row * a.runs) * 64 + threadIdx.x % 64) * 8;
-        const int left = int(min(a.cols - j, int64_t(8))), write = int(min(a.to_cols - j, int64_t(8)));
-        if (write <= 0) continue;
-        float v[8] = {};
-        if (left > 0) {
-            const i8x8 q = load_codes(a.codes + row * a.codes_stride + j, left);
-            const float scale = scale_value(a.scales[row * a.scales_stride + j / FSDP_STEP_GROUP]);
+    for_items(a.items, a.runs, a.to_cols, [&](const Place (&at)[kTogether]) {
+        i8x8 q[kTogether];
+        float scale[kTogether];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = c < left ? float(q[c]) * scale : 0.f;
+        for (int u = 0; u < kTogether; ++u) {
+            const int left = at[u].left > 0 ? int(min(a.cols - at[u].j, int64_t(8))) : 0;
+            const int8_t* const codes = a.codes + at[u].row * a.codes_stride + at[u].j;
+            if (left >= 8) q[u] = load_codes_once(codes);
+            else q[u] = load_codes(codes, left);
+            scale[u] = left > 0 ? scale_value(a.scales[at[u].row * a.scales_stride + at[u].j / FSDP_STEP_GROUP]) : 0.f;
         }
-        store_some(static_cast<T*>(a.x) + row * a.x_stride + j, write, v);
-    }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = at[u].j + c < a.cols ? float(q[u][c]) * scale[u] : 0.f;
+            if (at[u].left > 0) store_some(static_cast<T*>(a.x) + at[u].row * a.x_stride + at[u].j, at[u].left, v);
+        }
+    });
 }
 
 fsdp_status check(int64_t rows, int64_t cols, fsdp_dtype dtype) {
@@ -78,7 +115,7 @@ fsdp_status restore(const void* codes, int64_t codes_stride, const void* scales,
     if (items == 0) return FSDP_OK;
     const RestoreArgs k{static_cast<const int8_t*>(codes), static_cast<const uint8_t*>(scales), x, codes_stride, scales_stride,
                         x_stride, cols, to_cols, runs, items};
-    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4), 1 << 16)));
+    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4 * kTogether), 1 << 16)));
     return with_type(dtype, [&](auto type) { return launch(restore_kernel<decltype(type)>, k, grid, 256, stream); });
 }
 
@@ -100,7 +137,7 @@ extern "C" fsdp_status fsdp_step_save(const fsdp_step_save_args* args, hipStream
     const int64_t runs = ceil_div(a.cols, 512), items = a.rows * runs;
     const SaveArgs k{a.x, static_cast<int8_t*>(a.codes), static_cast<uint8_t*>(a.scales), a.x_stride, a.codes_stride,
                      a.scales_stride, a.cols, runs, items};
-    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4), 1 << 16)));
+    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4 * kTogether), 1 << 16)));
     return with_type(a.dtype, [&](auto type) { return launch(save_kernel<decltype(type)>, k, grid, 256, stream); });
 }
 
