@@ -37,6 +37,17 @@ constexpr Form kForms32[] = {
     {64, 128, 4, 1, 0.95, 0.95, 3.5},
 };
 
+// The forms that a library has, the smallest last, and those that the rest of a last round
+// may go in.
+struct Forms {
+    const Form* all;
+    int count;
+    const Form* rest;
+    int rests;
+};
+constexpr Forms kLinear16{kForms16, 5, kForms16 + 1, 1}, kLinear32{kForms32, 2, nullptr, 0};
+inline const Forms& linear_forms(fsdp_dtype dtype) { return dtype == FSDP_DTYPE_F32 ? kLinear32 : kLinear16; }
+
 // How one product is run.
 struct Cut {
     const Form* form = nullptr;      // NULL: row_kernel
@@ -95,19 +106,18 @@ double rounds_time(const Form& form, int64_t groups, int64_t steps, int cus) {
 // end, and the rest of out takes tiles of 128 x 128 in a second launch (3 us): bf16
 // 6144 x 6144 x 4096 takes 281 us instead of 301, 14336 x 4096 with k = 8192 746
 // instead of 791.  (Smaller tiles for the rest: 334 instead of 300 us at 5000^3.)
-// `smallest`: tiles of 64 x 64 are built too; `rows_too`: up to four rows go without tiles.
-Cut choose(const Shape& s, int cus, bool smallest = true, bool rows_too = true) {
+// `rows_too`: up to four rows go without tiles.
+Cut choose(const Shape& s, int cus, const Forms& set, bool rows_too = true) {
     Cut best;
     if (rows_too && row_form(s)) return best;
     const bool wide = s.dtype == FSDP_DTYPE_F32;
-    const Form* const forms = wide ? kForms32 : kForms16;
     const int step_k = wide ? 32 : 64;
     const int64_t steps = std::max<int64_t>(1, ceil_div(s.k, step_k));
     const double read = double(elem_bytes(s.dtype)) * (double(s.m) * double(s.k) + double(s.n) * double(s.k));
     const double joining = double(s.m) * double(s.n) * 8 / 5e6;
     double least = 0;
-    for (int f = 0; f < (wide ? 2 : smallest ? 5 : 4); ++f) {
-        const Form& form = forms[f];
+    for (int f = 0; f < set.count; ++f) {
+        const Form& form = set.all[f];
         if (!reaches(form, s)) continue;
         const int64_t tiles = ceil_div(s.m, form.tile_m) * ceil_div(s.n, form.tile_n);
         for (int parts = 1; parts <= 16; ++parts) {
@@ -128,8 +138,8 @@ Cut choose(const Shape& s, int cus, bool smallest = true, bool rows_too = true) 
             }
         }
     }
-    if (wide || s.m == 0 || s.n == 0) return best;
-    const Form &big = forms[0], &small = forms[1];
+    if (set.rests == 0 || s.m == 0 || s.n == 0) return best;
+    const Form& big = set.all[0];
     if (!reaches(big, s)) return best;
     const int64_t down = ceil_div(s.m, big.tile_m), across = ceil_div(s.n, big.tile_n);
     for (const bool rows : {true, false}) {
@@ -137,16 +147,19 @@ Cut choose(const Shape& s, int cus, bool smallest = true, bool rows_too = true) 
         const int64_t other = rows ? across : down, taken = down * across / cus * cus / other;
         const int64_t at = taken * (rows ? big.tile_m : big.tile_n), m = rows ? s.m - at : s.m, n = rows ? s.n : s.n - at;
         if (taken == 0 || m <= 0 || n <= 0) continue;
-        const double time = rounds_time(big, taken * other, steps, cus) + 3.0 +
-                            rounds_time(small, ceil_div(m, small.tile_m) * ceil_div(n, small.tile_n), steps, cus);
-        if (time >= least) continue;
-        least = time;
-        best = Cut{};
-        best.form = &big;
-        best.part_k = steps * step_k;
-        best.rest = &small;
-        best.rest_rows = rows;
-        best.rest_at = at;
+        for (int f = 0; f < set.rests; ++f) {
+            const Form& small = set.rest[f];
+            const double time = rounds_time(big, taken * other, steps, cus) + 3.0 +
+                                rounds_time(small, ceil_div(m, small.tile_m) * ceil_div(n, small.tile_n), steps, cus);
+            if (time >= least) continue;
+            least = time;
+            best = Cut{};
+            best.form = &big;
+            best.part_k = steps * step_k;
+            best.rest = &small;
+            best.rest_rows = rows;
+            best.rest_at = at;
+        }
     }
     return best;
 }
@@ -171,9 +184,9 @@ bool on_grid(const Source& o, fsdp_dtype dtype) {
 int64_t laid_stride(const Source& o, fsdp_dtype dtype) { return on_grid(o, dtype) ? o.stride : lined(o.cols, dtype); }
 
 // Whether any form reaches the operands (row_kernel reaches all of its).
-fsdp_status check_reach(const Shape& s, bool smallest = true, bool rows_too = true) {
+fsdp_status check_reach(const Shape& s, const Forms& set, bool rows_too = true) {
     if (s.m == 0 || s.n == 0 || (rows_too && row_form(s))) return FSDP_OK;
-    if (s.dtype == FSDP_DTYPE_F32 ? reaches(kForms32[1], s) : reaches(kForms16[smallest ? 4 : 3], s)) return FSDP_OK;
+    if (reaches(set.all[set.count - 1], s)) return FSDP_OK;
     return fail(FSDP_ERR_OVERFLOW, "a tile's rows of an operand of %lld x %lld, %lld x %lld do not lie within 2^31 bytes",
                 (long long)s.m, (long long)s.k, (long long)s.n, (long long)s.k);
 }

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
 
 // Adds a product's needs to those of `bytes`.
 Cut plan(const Shape& s, const Source& a, const Source& b, int cus, int64_t bytes) {
-    Cut c = choose(s, cus);
+    Cut c = choose(s, cus, linear_forms(s.dtype));
     c.bytes = bytes;
     if (!c.form || s.m == 0 || s.n == 0 || s.k == 0) return c;
     const auto take = [&](int64_t n) {
@@ -301,10 +301,10 @@ struct GradParts {
 fsdp_status check_reach(const fsdp_linear_grad_args& a) {
     const Source dz = grad_dz(a, !dz_is_dout(a), nullptr);
     if (a.dx) {
-        const fsdp_status st = check_reach(grad_shape(a, false, dz, {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false}));
+        const fsdp_status st = check_reach(grad_shape(a, false, dz, {a.weight, a.n, a.k, row_stride(a.n, a.k, a.weight_stride), false}), linear_forms(a.dtype));
         if (st != FSDP_OK) return st;
     }
-    return a.dweight ? check_reach(grad_shape(a, true, dz, {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false})) : FSDP_OK;
+    return a.dweight ? check_reach(grad_shape(a, true, dz, {a.x, a.m, a.k, row_stride(a.m, a.k, a.x_stride), false}), linear_forms(a.dtype)) : FSDP_OK;
 }
 
 GradParts parts_of(const fsdp_linear_grad_args& a, int cus, char* ws) {
@@ -349,7 +349,7 @@ extern "C" fsdp_status fsdp_block_linear_workspace(const fsdp_linear_args* args,
     clear_error();
     if (!args || !bytes) return fail(FSDP_ERR_INVALID, "args or bytes is NULL");
     fsdp_status st = check_linear(*args);
-    if (st == FSDP_OK) st = check_reach(forward_shape(*args));
+    if (st == FSDP_OK) st = check_reach(forward_shape(*args), linear_forms(args->dtype));
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;
@@ -363,7 +363,7 @@ extern "C" fsdp_status fsdp_block_linear(const fsdp_linear_args* args, void* wor
     if (!args) return fail(FSDP_ERR_INVALID, "args is NULL");
     const fsdp_linear_args& a = *args;
     fsdp_status st = check_linear(a);
-    if (st == FSDP_OK) st = check_reach(forward_shape(a));
+    if (st == FSDP_OK) st = check_reach(forward_shape(a), linear_forms(a.dtype));
     if (st != FSDP_OK) return st;
     const int cus = cu_count(&st);
     if (cus == 0) return st;

@@ -215,6 +215,22 @@ __global__ __launch_bounds__(256) void saved_slope_kernel(const SavedSlopeArgs a
 
 int64_t row_stride(int64_t rows, int64_t cols, int64_t stride) { return rows > 1 ? stride : round_up(cols, 8); }
 
+// The forms of a product, as block_cut.h has them: in 16 bits those of step_tile.h (`steps` is
+// their ring), then block_product.h's; a forward product has none of 64 x 64. Times from a round of
+// 256 workgroups (or 512 of two on a CU) at k = 2560 and 10240, the three kinds of product within
+// 5 % of each other. (Tiles of 128 x 256 take 0.83 to 0.93 us a step, two of 128 x 128 on a CU
+// the same: they are not built.)
+constexpr Form kRings[] = {
+    {256, 256, 5, 1, 1.25, 1.45, 7.0},
+    {128, 128, 5, 2, 0.50, 0.92, 5.0},
+    {128, 128, 10, 1, 0.42, 0.45, 4.5},
+    {64, 128, 4, 1, 0.28, 0.32, 4.0},
+    {64, 64, 8, 1, 0.16, 0.21, 4.0},
+};
+constexpr Forms kForward16{kRings, 4, kRings + 1, 1}, kGrad16{kRings, 5, kRings + 1, 1};
+const Forms& forward_forms(fsdp_dtype dtype) { return dtype == FSDP_DTYPE_F32 ? kLinear32 : kForward16; }
+const Forms& grad_forms(fsdp_dtype dtype) { return dtype == FSDP_DTYPE_F32 ? kLinear32 : kGrad16; }
+
 // A product's launches: `p` has its operands and epilogue, `c` says how.
 template <typename Kind>
 fsdp_status launch_pair(const PairProduct& p, const Form& f, fsdp_dtype dtype, hipStream_t stream) {
@@ -229,7 +245,7 @@ fsdp_status launch_pair(const PairProduct& p, const Form& f, fsdp_dtype dtype, h
         if constexpr (kSmallest)
             if (f.tile_n == 64) return launch(pair_kernel<T, Kind, 64, 64, 8>, p, grid, 256, stream);
         if (f.tile_m == 64) return launch(pair_kernel<T, Kind, 64, 128, 4>, p, grid, 256, stream);
-        return f.steps == 2 ? launch(ring_kernel<T, Kind, 128, 5>, p, grid, 256, stream)
+        return f.steps == 5 ? launch(ring_kernel<T, Kind, 128, 5>, p, grid, 256, stream)
                             : launch(ring_kernel<T, Kind, 128, 10>, p, grid, 256, stream);
     };
     return dtype == FSDP_DTYPE_BF16 ? of(bf16(0.f)) : of(f16(0.f));
@@ -341,13 +357,13 @@ Forward forward_of(const fsdp_step_gated_args& a) {
 }
 
 fsdp_status check_reach(const fsdp_step_gated_args& a, const Forward& f) {
-    return by_rows(a, f.shape) ? FSDP_OK : check_reach(f.shape, false, false);
+    return by_rows(a, f.shape) ? FSDP_OK : check_reach(f.shape, forward_forms(a.dtype), false);
 }
 
 void plan_forward(const fsdp_step_gated_args& a, int cus, Forward& f) {
     Room room;
     if (a.m > 0 && a.n > 0 && !by_rows(a, f.shape)) {
-        f.cut = choose(f.shape, cus, false, false);
+        f.cut = choose(f.shape, cus, forward_forms(a.dtype), false);
         const Source* const from[3] = {&f.x, &f.gate, &f.up};
         for (int w = 0; w < 3; ++w)
             if (!on_grid(*from[w], a.dtype)) f.pad[w] = room.laid(*from[w], a.dtype);
@@ -402,8 +418,8 @@ void shape_grad(Grad& g) {
 
 fsdp_status check_reach(const Grad& g) {
     fsdp_status st = FSDP_OK;
-    if (g.dx && g.n > 0) st = check_reach(g.dx_shape);
-    return st == FSDP_OK && g.dweight ? check_reach(g.dw_shape) : st;
+    if (g.dx && g.n > 0) st = check_reach(g.dx_shape, grad_forms(g.dtype));
+    return st == FSDP_OK && g.dweight ? check_reach(g.dw_shape, grad_forms(g.dtype)) : st;
 }
 
 void plan_grad(Grad& g, int cus, bool dz, bool sums) {
@@ -424,7 +440,7 @@ void plan_grad(Grad& g, int cus, bool dz, bool sums) {
     // The two products follow each other on the stream: they share what each needs.
     Room first = room, second = room;
     if (g.dx) {
-        g.dx_cut = choose(g.dx_shape, cus);
+        g.dx_cut = choose(g.dx_shape, cus, grad_forms(g.dtype));
         if (g.m > 0 && g.n > 0) {
             if (!joined(g))
                 for (int w = 0; w < (g.two ? 2 : 1); ++w) g.pad[w] = first.laid(g.weight[w], g.dtype);
@@ -432,7 +448,7 @@ void plan_grad(Grad& g, int cus, bool dz, bool sums) {
         }
     }
     if (g.dweight) {
-        g.dw_cut = choose(g.dw_shape, cus);
+        g.dw_cut = choose(g.dw_shape, cus, grad_forms(g.dtype));
         if (g.m > 0 && g.n > 0) add_parts(g.dw_cut, g.dw_shape, round_up(g.k, 8), second);
     }
     g.bytes = std::max(first.bytes, second.bytes);
