@@ -225,12 +225,14 @@ fsdp_status run(const fsdp_step_policy_args* args, bool backward, hipStream_t st
     fsdp_status found = FSDP_OK;
     const int cus = cu_count(&found);
     if (cus == 0) return found;
-    // As the distillation loss, whose passes over the logits are the same: 256 threads that hold a row
-    // in four units each; few rows, 1024 threads; else 256, or 512 for a long row that is read twice.
+    // A wave that holds a row whole: no wait between waves (6669 x 1847 in bf16, loss and gradient:
+    // 19.1 us instead of 29.5). Else as the distillation loss, whose passes over the logits are the
+    // same: few rows, 1024 threads; 256, or 512 for a long row that is read twice.
     const int64_t units = ceil_div(a.vocab, 16 / elem_bytes(a.dtype));
     const bool twice = !backward && a.dlogits;
     const auto of = [&](auto type) {
         using T = decltype(type);
+        if (units <= 8 * 64) return launch(policy_kernel<T, 64, 8>, k, grid, 64, stream);
         if (units <= 4 * 256) return launch(policy_kernel<T, 256, 4>, k, grid, 256, stream);
         if (t <= cus) return launch(policy_kernel<T, 1024, 8>, k, grid, 1024, stream);
         if (!twice || units <= 4096) return launch(policy_kernel<T, 256, 8>, k, grid, 256, stream);

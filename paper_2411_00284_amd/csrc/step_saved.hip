@@ -2,7 +2,7 @@
 //
 // Bound by HBM: bf16 moves 3.03 bytes an element either way.  A lane takes eight
 // columns, so that four lanes hold a group and find its largest magnitude by two
-// exchanges in the quad; a wave takes a run of 512 columns of a row.
+// exchanges in the quad.
 
 #include "step_saved.h"
 
@@ -11,41 +11,62 @@
 namespace fsdp_block {
 namespace {
 
-struct SaveArgs {
-    const void* x;
-    int8_t* codes;
-    uint8_t* scales;
-    int64_t x_stride, codes_stride, scales_stride, cols, runs, items;
-};
-
-// Items of a wave: kTogether neighbouring ones, all asked for before the first is worked on.
-// Each is a place in the matrix: this lane's eight columns.
+// A lane takes eight columns, a quad a group of 32. Items of a wave are 64 times eight columns,
+// kTogether neighbouring ones, all asked for before the first is worked on: a run of 512 columns of
+// a row, `runs` to a row; or (runs is 0) whole groups of one row after the other, `per` times
+// eight columns to a row: of rows of less than 512 columns, whose runs would leave lanes idle.
 constexpr int kTogether = 4;
+struct Places {
+    int64_t rows, cols, runs, per, items;
+};
+Places places(int64_t rows, int64_t cols) {
+    const int64_t per = ceil_div(cols, FSDP_STEP_GROUP) * 4;
+    return per < 64 ? Places{rows, cols, 0, per, ceil_div(rows * per, 64)} : Places{rows, cols, ceil_div(cols, 512), 0, rows * ceil_div(cols, 512)};
+}
 struct Place {
     int64_t row, j;
     int left;                        // columns from j on; 0 and less: none
 };
 template <typename F>
-__device__ __forceinline__ void for_items(int64_t items, int64_t runs, int64_t cols, F f) {
-    for (int64_t first = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * kTogether; first < items; first += int64_t(gridDim.x) * 4 * kTogether) {
+__device__ __forceinline__ void for_items(const Places& p, F f) {
+    for (int64_t first = (int64_t(blockIdx.x) * 4 + threadIdx.x / 64) * kTogether; first < p.items; first += int64_t(gridDim.x) * 4 * kTogether) {
         Place at[kTogether];
-        int64_t row = first / runs, run = first - row * runs;
+        if (p.runs) {
+            int64_t row = first / p.runs, run = first - row * p.runs;
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            at[u] = {row, (run * 64 + threadIdx.x % 64) * 8, 0};
-            at[u].left = first + u < items ? int(min(cols - at[u].j, int64_t(8))) : -1;
-            if (++run == runs) {
-                run = 0;
-                ++row;
+            for (int u = 0; u < kTogether; ++u) {
+                at[u] = {row, (run * 64 + threadIdx.x % 64) * 8, 0};
+                at[u].left = first + u < p.items ? int(min(p.cols - at[u].j, int64_t(8))) : -1;
+                if (++run == p.runs) {
+                    run = 0;
+                    ++row;
+                }
+            }
+        } else {
+            const int64_t row0 = first * 64 / p.per;
+            const uint32_t unit0 = uint32_t(first * 64 - row0 * p.per) + threadIdx.x % 64, per = uint32_t(p.per);
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) {
+                const uint32_t down = (unit0 + 64 * u) / per;
+                at[u] = {row0 + down, int64_t(unit0 + 64 * u - down * per) * 8, 0};
+                at[u].left = at[u].row < p.rows ? int(min(p.cols - at[u].j, int64_t(8))) : -1;
             }
         }
         f(at);
     }
 }
 
+struct SaveArgs {
+    const void* x;
+    int8_t* codes;
+    uint8_t* scales;
+    int64_t x_stride, codes_stride, scales_stride;
+    Places places;
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void save_kernel(const SaveArgs a) {
-    for_items(a.items, a.runs, a.cols, [&](const Place (&at)[kTogether]) {
+    for_items(a.places, [&](const Place (&at)[kTogether]) {
         Eight<T> in[kTogether];
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
@@ -68,13 +89,14 @@ struct RestoreArgs {
     const int8_t* codes;
     const uint8_t* scales;
     void* x;
-    int64_t codes_stride, scales_stride, x_stride, cols, to_cols, runs, items;
+    int64_t codes_stride, scales_stride, x_stride, cols;
+    Places places;                   // of x, with its zeros after `cols`
 };
 
 // Columns cols .. to_cols - 1 become zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void restore_kernel(const RestoreArgs a) {
-    for_items(a.items, a.runs, a.to_cols, [&](const Place (&at)[kTogether]) {
+    for_items(a.places, [&](const Place (&at)[kTogether]) {
         i8x8 q[kTogether];
         float scale[kTogether];
 #pragma unroll
@@ -111,11 +133,11 @@ fsdp_status with_type(fsdp_dtype dtype, F f) {
 
 fsdp_status restore(const void* codes, int64_t codes_stride, const void* scales, int64_t scales_stride, void* x, int64_t x_stride,
                     int64_t rows, int64_t cols, int64_t to_cols, fsdp_dtype dtype, hipStream_t stream) {
-    const int64_t runs = ceil_div(to_cols, 512), items = rows * runs;
-    if (items == 0) return FSDP_OK;
+    if (rows == 0 || to_cols == 0) return FSDP_OK;
+    const Places p = places(rows, to_cols);
     const RestoreArgs k{static_cast<const int8_t*>(codes), static_cast<const uint8_t*>(scales), x, codes_stride, scales_stride,
-                        x_stride, cols, to_cols, runs, items};
-    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4 * kTogether), 1 << 16)));
+                        x_stride, cols, p};
+    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(p.items, 4 * kTogether), 1 << 16)));
     return with_type(dtype, [&](auto type) { return launch(restore_kernel<decltype(type)>, k, grid, 256, stream); });
 }
 
@@ -134,10 +156,10 @@ extern "C" fsdp_status fsdp_step_save(const fsdp_step_save_args* args, hipStream
     c.add("codes", a.codes, a.rows, a.cols, a.codes_stride, kBytes, true, true);
     c.add("scales", a.scales, a.rows, ceil_div(a.cols, FSDP_STEP_GROUP), a.scales_stride, kBytes, true, true);
     if ((st = c.done()) != FSDP_OK || a.rows == 0 || a.cols == 0) return st;
-    const int64_t runs = ceil_div(a.cols, 512), items = a.rows * runs;
+    const Places p = places(a.rows, a.cols);
     const SaveArgs k{a.x, static_cast<int8_t*>(a.codes), static_cast<uint8_t*>(a.scales), a.x_stride, a.codes_stride,
-                     a.scales_stride, a.cols, runs, items};
-    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(items, 4 * kTogether), 1 << 16)));
+                     a.scales_stride, p};
+    const dim3 grid(unsigned(std::min<int64_t>(ceil_div(p.items, 4 * kTogether), 1 << 16)));
     return with_type(a.dtype, [&](auto type) { return launch(save_kernel<decltype(type)>, k, grid, 256, stream); });
 }
 
