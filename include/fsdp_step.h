@@ -114,7 +114,7 @@ typedef struct fsdp_step_gated_grad_args {
     int64_t m, n, k;
     fsdp_dtype dtype;
     fsdp_activation activation;
-    const void* dout;
+    const void* dout;              /* with any output */
     const void* x;                 /* or NULL without the weights' gradients */
     const void* x_scales;          /* or NULL */
     const void* gate_weight;       /* or NULL without dx */
@@ -195,7 +195,7 @@ typedef struct fsdp_step_policy_args {
     float clip_low;                /* 0 .. 1 */
     float clip_high;               /* >= 0, may be infinite */
     float kl_weight;               /* finite; needs ref_logp unless 0 */
-    float temperature;             /* tau > 0, finite */
+    float temperature;             /* tau >= 2^-126, finite */
     const void* logits;            /* [tokens, vocab] */
     const void* actions;           /* [tokens] */
     const float* old_logp;         /* [tokens] */

@@ -542,7 +542,7 @@ fsdp_status check_gated_grad(const fsdp_step_gated_grad_args& a) {
     if (a.n > 0 && !a.dgate_weight != !a.dup_weight) return fail(FSDP_ERR_INVALID, "dgate_weight and dup_weight go together");
     if (a.m > 0 && a.n > 0 && !a.gate_scales != !a.up_scales) return fail(FSDP_ERR_INVALID, "gate_scales and up_scales go together");
     Checked c;
-    c.add_in_place("dout", a.dout, a.m, a.n, a.dout_stride, a.dtype, a.dx || a.dgate_weight);
+    c.add_in_place("dout", a.dout, a.m, a.n, a.dout_stride, a.dtype, any);
     add_kept(c, "x", "x_scales", a.x, a.x_scales, a.m, a.k, a.x_stride, a.x_scales_stride, a.dtype, a.dgate_weight && a.n > 0, false);
     c.add("gate_weight", a.gate_weight, a.n, a.k, a.gate_weight_stride, a.dtype, a.dx && a.m > 0);
     c.add("up_weight", a.up_weight, a.n, a.k, a.up_weight_stride, a.dtype, a.dx && a.m > 0);

@@ -60,7 +60,8 @@ __device__ __forceinline__ void token_loss(const PolicyArgs& a, int64_t row, dou
     }
 }
 
-// kHeld units per thread stay in registers.
+// kHeld units per thread stay in registers, the others are streamed kStream at a time.
+constexpr int kStream = 4;
 template <typename T, int kThreads, int kHeld>
 __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(const PolicyArgs a) {
     constexpr int kWaves = kThreads / 64, n = Unit<T>::n;
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
     __shared__ float weight_of, at_action;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, vocab = a.vocab, units = vocab / n;
     const int single = units * n + t;                           // this thread's element after the units
-    const float c = fminf(kLog2e / a.tau, FLT_MAX);             // finite for a subnormal tau: 0 c is 0
+    const float c = fminf(kLog2e / a.tau, FLT_MAX);             // finite for the smallest tau: 0 c is 0
     const double per_tau = 1.0 / double(a.tau), ln2 = 0.6931471805599453;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         const T* const s = static_cast<const T*>(a.logits) + row * a.logits_stride;
@@ -101,10 +102,10 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
         if (!a.lse_in) {
 #pragma unroll
             for (int u = 0; u < kHeld / 2; ++u) add_units(x, held[u], c);
-            for (int j = t + kHeld * kThreads; j < units; j += kTogether * kThreads) {
-                Unit<T> u[kTogether];
+            for (int j = t + kHeld * kThreads; j < units; j += kStream * kThreads) {
+                Unit<T> u[kStream];
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) u[k].load(s, j + k * kThreads, units);
+                for (int k = 0; k < kStream; ++k) u[k].load(s, j + k * kThreads, units);
                 add_units(x, u, c);
             }
             x.join(lone, lone == -INFINITY ? 0.f : 1.f, c);
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
             const double logp = a.lse_in ? double(picked) * per_tau - double(a.lse_in[row]) : (double(picked) - double(x.m)) * per_tau - log_sum;
             float loss, slope;
             token_loss(a, row, logp, loss, slope);
-            const float weight = gradient ? a.dloss[row] * slope * float(per_tau) : 0.f;
+            const float weight = gradient ? float(double(a.dloss[row]) * double(slope) * per_tau) : 0.f;
             const float action_slope = weight * -expm1f(float(logp));      // 1 - q, with no difference of the two
             if (lane == 0) {
                 if (a.loss) a.loss[row] = loss;
@@ -170,12 +171,12 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
             };
 #pragma unroll
             for (int u = 0; u < kHeld; ++u) put(held[u / 2][u % 2], t + u * kThreads);
-            for (int j = t + kHeld * kThreads; j < units; j += kTogether * kThreads) {
-                Unit<T> u[kTogether];
+            for (int j = t + kHeld * kThreads; j < units; j += kStream * kThreads) {
+                Unit<T> u[kStream];
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) u[k].template load<true>(s, j + k * kThreads, units);
+                for (int k = 0; k < kStream; ++k) u[k].template load<true>(s, j + k * kThreads, units);
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) put(u[k], j + k * kThreads);
+                for (int k = 0; k < kStream; ++k) put(u[k], j + k * kThreads);
             }
             if (single < vocab) ds[single] = single == action ? T(at_action) : slope(lone);
         }
@@ -192,8 +193,9 @@ fsdp_status run(const fsdp_step_policy_args* args, bool backward, hipStream_t st
     if (a.vocab > INT32_MAX - (1 << 16)) return fail(FSDP_ERR_OVERFLOW, "vocab does not fit 31 bits");
     if (!known_dtype(a.dtype)) return fail(FSDP_ERR_INVALID, "unknown dtype");
     if (a.actions_64 != 0 && a.actions_64 != 1) return fail(FSDP_ERR_INVALID, "actions_64 must be 0 or 1");
-    if (!(a.temperature > 0.f) || !__builtin_isfinite(a.temperature))
-        return fail(FSDP_ERR_INVALID, "temperature must be positive and finite");
+    // A gradient is of the size of 1 / temperature.
+    if (!(a.temperature >= FLT_MIN) || !__builtin_isfinite(a.temperature))
+        return fail(FSDP_ERR_INVALID, "temperature must be positive, normal and finite");
     if (!(a.clip_low >= 0.f) || a.clip_low > 1.f) return fail(FSDP_ERR_INVALID, "clip_low must be in 0 .. 1");
     if (!(a.clip_high >= 0.f)) return fail(FSDP_ERR_INVALID, "clip_high must not be negative");
     if (!__builtin_isfinite(a.kl_weight)) return fail(FSDP_ERR_INVALID, "kl_weight must be finite");

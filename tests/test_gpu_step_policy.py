@@ -224,6 +224,25 @@ def test_rows(vocab):
         assert torch.equal(back.cpu().isnan(), dl.isnan()) and not back[[0, 1, 3, 7, 8, 9, 10, 11]].any()
 
 
+def test_small_temperatures():
+    """Near one-hot distributions: 0 and 1 for probabilities, gradients of the
+    size of 1 / temperature, nothing NaN."""
+    tokens, vocab = 6, 300
+    for dtype in (torch.bfloat16, torch.float32):
+        logits, actions, _, adv, _, dloss = make(101, tokens, vocab, dtype)
+        actions[:3] = logits[:3].float().argmax(1)
+        logits[0, actions[0]] += 1
+        for tau in (1e-3, 1e-20, 2.0 ** -126):
+            logp = ((logits.double() - logits.double().max(1, keepdim=True).values) / tau)
+            logp = (logp - torch.logsumexp(logp, 1, keepdim=True)).gather(1, actions[:, None])[:, 0]
+            old = logp.clamp(min=-80).float()
+            outs = [torch.empty(tokens, device="cuda") for _ in range(2)]
+            dl = torch.empty(tokens, vocab, dtype=dtype, device="cuda")
+            policy_loss(logits.cuda(), actions.cuda(), old.cuda(), adv.cuda(), *outs, temperature=tau, dloss=dloss.cuda(), dlogits=dl)
+            assert not any(bool(v.isnan().any()) for v in (*outs, dl)), (dtype, tau)
+            assert abs(float(outs[1][0])) < 1e-6                       # the action that stands out: probability 1
+
+
 def test_past_the_clip():
     """Four rows on each side of both borders: the gradient is zero where a
     larger gain is clipped, and only there."""

@@ -145,6 +145,7 @@ DW = dict(dgate_weight=at(9), dup_weight=at(10), dgate_weight_stride=8, dup_weig
     (dict(activation=-1), INVALID, "activation"),
     (dict(DX, gate=None), INVALID, "gate is NULL"),
     (dict(DX, dout=None), INVALID, "dout is NULL"),
+    (dict(out=at(8), out_stride=64, dout=None), INVALID, "dout is NULL"),
     (dict(DX, gate_weight=None), INVALID, "gate_weight is NULL"),
     (dict(DW, x=None), INVALID, "x is NULL"),
     (dict(dgate_weight=at(9), dgate_weight_stride=8), INVALID, "go together"),
@@ -189,6 +190,7 @@ POLICY = dict(tokens=4, vocab=100, temperature=1, clip_low=0.2, clip_high=0.2, l
     (dict(actions_64=2), INVALID, "actions_64"),
     (dict(temperature=0), INVALID, "temperature"),
     (dict(temperature=math.inf), INVALID, "temperature"),
+    (dict(temperature=1e-40), INVALID, "temperature"),
     (dict(clip_low=1.5), INVALID, "clip_low"),
     (dict(clip_low=math.nan), INVALID, "clip_low"),
     (dict(clip_high=-1), INVALID, "clip_high"),
