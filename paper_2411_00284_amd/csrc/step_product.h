@@ -283,7 +283,7 @@ struct JoinedStream : Stream<T, kRows, true> {
     }
 };
 
-// eight columns of a row to their place.
+// Eight columns of a row to their place.
 template <typename Kind>
 struct Plain : OneMatrix {
     template <typename T, int kWide, typename Place, typename Pieces>

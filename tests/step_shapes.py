@@ -16,7 +16,7 @@ ROWS = [(d, m, *s) for d in ("bf16", "f16", "f32") for m in (1, 2, 3, 4) for s i
 # m, n, k for each form of the gradient's products.
 GRADIENT_16 = [(3063, 200, 1288), (1976, 164, 4372), (9336, 136, 136), (264, 4700, 136), (88, 264, 8504), (200, 600, 300), (64, 4096, 256),
                (4096, 60, 500), (8192, 32, 256), (328, 1000, 4372)]
-GRADIENT_32 = [(5896, 100, 272), (70, 150, 100), (61, 1050, 250), (2100, 61, 125), (200, 3000, 272)]
+GRADIENT_32 = [(5896, 100, 272), (200, 260, 4204), (1000, 470, 1204), (70, 150, 100), (61, 1050, 250), (2100, 61, 125), (200, 3000, 272)]
 GRADIENT = [(d, s) for d in ("bf16", "f16", "f32") for s in (GRADIENT_32 if d == "f32" else GRADIENT_16)]
 
 # tokens, vocabulary: rows that a wave holds whole, that 256 threads do, few tokens, a micro-batch of long rows, and of longer ones.
