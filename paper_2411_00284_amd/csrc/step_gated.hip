@@ -255,13 +255,14 @@ constexpr Form kRings[] = {
 };
 // fp32, from products of 2048 x 1024 x 688 to 5000 x 2500 x 1500. A gradient's small tiles are those
 // of 64 x 64, two on a CU: the weights' gradients of 2048 x 688 -> 1024 take 67 us instead of 74 in
-// tiles of 64 x 128, of 59 x 28672 -> 256 the whole call 114 instead of 164.
+// tiles of 64 x 128, of 59 x 28672 -> 256 the whole call 114 instead of 164. A linear layer's gradient
+// has the forms that it has without 8 bits, and so its bits.
 constexpr Form kForwards32[] = {{128, 128, 2, 2, 2.10, 4.15, 5.0}, {64, 128, 4, 1, 1.22, 1.28, 4.0}};
 constexpr Form kGrads32[] = {{128, 128, 2, 2, 2.10, 4.15, 5.0}, {64, 64, 4, 2, 0.58, 1.14, 3.5}};
 constexpr Forms kForward16{kRings, 4, kRings + 1, 1}, kGrad16{kRings, 5, kRings + 1, 1};
 constexpr Forms kForward32{kForwards32, 2, nullptr, 0}, kGrad32{kGrads32, 2, nullptr, 0};
 const Forms& forward_forms(fsdp_dtype dtype) { return dtype == FSDP_DTYPE_F32 ? kForward32 : kForward16; }
-const Forms& grad_forms(fsdp_dtype dtype) { return dtype == FSDP_DTYPE_F32 ? kGrad32 : kGrad16; }
+const Forms& grad_forms(fsdp_dtype dtype, bool two) { return dtype != FSDP_DTYPE_F32 ? kGrad16 : two ? kGrad32 : kLinear32; }
 
 // A product's launches: `p` has its operands and epilogue, `c` says how.
 template <typename Kind>
@@ -270,8 +271,9 @@ fsdp_status launch_pair(const PairProduct& p, const Form& f, fsdp_dtype dtype, h
     const dim3 grid(unsigned(ceil_div(p.m - p.first_i, f.tile_m) * ceil_div(p.n - p.first_j, f.tile_n) * p.count));
     if (dtype == FSDP_DTYPE_F32) {
         if (f.tile_m == 128) return launch(pair_kernel<float, Kind, 128, 128, 2>, p, grid, 256, stream);
-        if constexpr (kSmallest) return launch(pair_kernel<float, Kind, 64, 64, 4>, p, grid, 256, stream);
-        else return launch(pair_kernel<float, Kind, 64, 128, 4>, p, grid, 256, stream);
+        if constexpr (kSmallest)
+            if (f.tile_n == 64) return launch(pair_kernel<float, Kind, 64, 64, 4>, p, grid, 256, stream);
+        return launch(pair_kernel<float, Kind, 64, 128, 4>, p, grid, 256, stream);
     }
     const auto of = [&](auto type) {
         using T = decltype(type);
@@ -454,8 +456,8 @@ void shape_grad(Grad& g) {
 
 fsdp_status check_reach(const Grad& g) {
     fsdp_status st = FSDP_OK;
-    if (g.dx && g.n > 0) st = check_reach(g.dx_shape, grad_forms(g.dtype));
-    return st == FSDP_OK && g.dweight ? check_reach(g.dw_shape, grad_forms(g.dtype)) : st;
+    if (g.dx && g.n > 0) st = check_reach(g.dx_shape, grad_forms(g.dtype, g.two));
+    return st == FSDP_OK && g.dweight ? check_reach(g.dw_shape, grad_forms(g.dtype, g.two)) : st;
 }
 
 void plan_grad(Grad& g, int cus, bool dz, bool sums) {
@@ -476,7 +478,7 @@ void plan_grad(Grad& g, int cus, bool dz, bool sums) {
     // The two products follow each other on the stream: they share what each needs.
     Room first = room, second = room;
     if (g.dx) {
-        g.dx_cut = choose(g.dx_shape, cus, grad_forms(g.dtype));
+        g.dx_cut = choose(g.dx_shape, cus, grad_forms(g.dtype, g.two));
         if (g.m > 0 && g.n > 0) {
             if (!joined(g))
                 for (int w = 0; w < (g.two ? 2 : 1); ++w) g.pad[w] = first.laid(g.weight[w], g.dtype);
@@ -484,7 +486,7 @@ void plan_grad(Grad& g, int cus, bool dz, bool sums) {
         }
     }
     if (g.dweight) {
-        g.dw_cut = choose(g.dw_shape, cus, grad_forms(g.dtype));
+        g.dw_cut = choose(g.dw_shape, cus, grad_forms(g.dtype, g.two));
         if (g.m > 0 && g.n > 0) add_parts(g.dw_cut, g.dw_shape, round_up(g.k, 8), second);
     }
     g.bytes = std::max(first.bytes, second.bytes);

@@ -362,6 +362,23 @@ def test_8_bits_as_their_values():
         assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+@pytest.mark.parametrize("m,n,k", [(300, 1032, 328), (61, 250, 2100), (776, 72, 1287), (2100, 61, 125)])
+def test_linear_in_fp32_has_its_bits(m, n, k):
+    """A linear layer's gradient in fp32 goes in the same parts from 8 bits as from
+    the values they stand for."""
+    weight, dout = normal(1, n, k, dtype=torch.float32).cuda(), normal(2, m, n, dtype=torch.float32).cuda()
+    held = [Saved(normal(s, m, c, dtype=torch.float32)).c for s, c in ((3, k), (4, n))]
+    values = [torch.empty(h.codes.shape, device="cuda") for h in held]
+    for h, v in zip(held, values):
+        checkpoint_restore(h, v)
+    got = []
+    for x, pre in (held, values):
+        outs = {q: torch.empty(s, device="cuda") for q, s in (("dx", (m, k)), ("dweight", (n, k)))}
+        linear_backward(dout, x, weight, activation="silu", pre=pre, **outs)
+        got.append(list(outs.values()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_refusals():
     new = lambda *s: torch.full(s, 3, dtype=torch.bfloat16, device="cuda")  # noqa: E731
     x, gw, uw, out, gate, up = new(4, 64), new(32, 64), new(32, 64), new(4, 32), new(4, 32), new(4, 32)
