@@ -383,6 +383,7 @@ struct Fragments {
 // matrix B and one of out.
 struct OneMatrix {
     static constexpr bool kPair = false;         // tiles of kTileN / 2 columns of two matrices
+    static constexpr int kRun = 0;               // steps of fp32 after which their sum joins the others', 0: none
     template <typename T, int kTileN, bool kColumnsB>
     using B = Operand<T, kTileN, kColumnsB>;
     template <typename T, int kTileN, bool kColumnsB>
@@ -423,6 +424,20 @@ __device__ __forceinline__ void product_tile(const Args& p) {
     FA::lane_places(wi, pa);
     FB::lane_places(Kind::kPair ? wj / 2 : wj, pb);
     f32x16 acc[kA][kB] = {};
+    // fp32: a sum of few terms, and the sum of those; a term's rounding is then of a small sum.
+    constexpr bool kRuns = Kind::kRun > 0 && sizeof(T) == 4;
+    static_assert(Kind::kRun % kSteps == 0);
+    f32x16 sum[kRuns ? kA : 1][kRuns ? kB : 1] = {};
+    int run = 0;
+    const auto join = [&] {
+#pragma unroll
+        for (int x = 0; x < kA; ++x)
+#pragma unroll
+            for (int y = 0; y < kB; ++y) {
+                sum[x][y] += acc[x][y];
+                acc[x][y] = f32x16{};
+            }
+    };
 
     // Waits for this wave's loads, but for those of the last kLater steps, and
     // its LDS reads; then for the other waves.
@@ -499,6 +514,13 @@ __device__ __forceinline__ void product_tile(const Args& p) {
     fb[0].read(b0, pb, 0);
     // Steps past the end add zeros: the loop takes kSteps at a time.
     for (int64_t left = k1 - k0; left > 0; left -= kDeep * kSteps) {
+        if constexpr (kRuns) {
+            if (run == Kind::kRun) {
+                join();
+                run = 0;
+            }
+            run += kSteps;
+        }
         step(a0, b0, a1, b1);
         if constexpr (kSteps == 2) {
             step(a1, b1, a0, b0);
@@ -517,6 +539,11 @@ __device__ __forceinline__ void product_tile(const Args& p) {
         }
     }
     sync(std::integral_constant<int, 0>());                       // nothing more is written to LDS
+    if constexpr (kRuns)
+#pragma unroll
+        for (int x = 0; x < kA; ++x)
+#pragma unroll
+            for (int y = 0; y < kB; ++y) acc[x][y] += sum[x][y];
 
     // A wave passes its sums through its own piece of LDS, kTurn tiles at a time,
     // so that a lane gets eight neighbouring columns; every other four rows have

@@ -362,6 +362,29 @@ def test_8_bits_as_their_values():
         assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+def test_long_sums_in_fp32():
+    """Sums over many terms go in runs of 512.  Of random terms the sum of i is sqrt(i / n) of that
+    of n, and each addition off by at most 2^-24 of it: all additions of a run by 2^-24 sqrt(512 / 2),
+    of R runs by as much of the whole, and their sum by 2^-24 sqrt(R / 2) more."""
+    off = lambda got, want: float((got.double() - want).norm() / want.norm())  # noqa: E731
+    bound = lambda terms: 2.0**-24 * (256 + (terms + 511) // 512 / 2 + 1) ** 0.5  # noqa: E731
+    new = lambda s, *shape: normal(s, *shape, dtype=torch.float32).cuda()  # noqa: E731
+    m, n, k = 1910, 1024, 7864
+    x, gw, uw = new(1, m, k), new(2, n, k), new(3, n, k)
+    out, gate, up = (torch.empty(m, n, device="cuda") for _ in range(3))
+    gated_linear(x, gw, uw, out, activation="none", gate=gate, up=up)
+    assert off(gate, x.double() @ gw.double().t()) <= bound(k)
+    assert off(up, x.double() @ uw.double().t()) <= bound(k)
+    m, n, k = 4096, 1024, 1024
+    x, gw, uw, gate, up, dout = new(1, m, k), new(2, n, k), new(3, n, k), new(4, m, n), new(5, m, n), new(6, m, n)
+    dx, dg, du = torch.empty_like(x), torch.empty_like(gw), torch.empty_like(uw)
+    gated_linear_backward(dout, x, gw, uw, gate, up, activation="none", dx=dx, dgate_weight=dg, dup_weight=du)
+    first, second = (dout * up).double(), (dout * gate).double()
+    assert off(dg, first.t() @ x.double()) <= bound(m)
+    assert off(du, second.t() @ x.double()) <= bound(m)
+    assert off(dx, first @ gw.double() + second @ uw.double()) <= bound(2 * n)
+
+
 @pytest.mark.parametrize("m,n,k", [(300, 1032, 328), (61, 250, 2100), (776, 72, 1287), (2100, 61, 125)])
 def test_linear_in_fp32_has_its_bits(m, n, k):
     """A linear layer's gradient in fp32 goes in the same parts from 8 bits as from
