@@ -68,6 +68,63 @@ __device__ __forceinline__ void finish_pair(const PairProduct& p, int64_t i, int
 // fp32: runs of 512 k. One sum over k = 7864 is off by 1.6e-6 of the result (2-norm), in runs by
 // 4.1e-7; they cost 1 to 3 % (1910 x 1024 x 7864: 551 us, 537 without).
 constexpr int kRunSteps = 16;
+// As finish_pair, kApart, of several times eight columns that all exist: kDown rows 16 apart of kAcross
+// groups. Without branches of their own, so that their chains of instructions overlap where a SIMD
+// has one wave.
+template <typename T, int kDown, int kAcross>
+__device__ __forceinline__ void finish_whole(const PairProduct& p, int64_t i, int64_t j, const float (&g)[kDown][kAcross][8],
+                                             const float (&u)[kDown][kAcross][8]) {
+    const auto keep = [&](void* kept, uint8_t* scales, int64_t stride, int64_t scales_stride, const float (&z)[kDown][kAcross][8]) {
+        if (!kept) return;
+        if (scales) {
+            uint32_t byte[kDown][kAcross];
+#pragma unroll
+            for (int d = 0; d < kDown; ++d)
+#pragma unroll
+                for (int a = 0; a < kAcross; ++a) {
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) most = max(most, __builtin_bit_cast(uint32_t, z[d][a][c]) & 0x7fffffffu);
+                    byte[d][a] = scale_byte(group_max<true>(most));
+                }
+            int8_t* const codes = static_cast<int8_t*>(kept) + i * stride + j;
+#pragma unroll
+            for (int d = 0; d < kDown; ++d)
+#pragma unroll
+                for (int a = 0; a < kAcross; ++a)
+                    reinterpret_cast<AnyCodes*>(codes + 16 * d * stride + FSDP_STEP_GROUP * a)->v = codes_of(z[d][a], byte[d][a]);
+            if ((threadIdx.x & 48) != 0) return;
+            uint8_t* const scale = scales + i * scales_stride + j / FSDP_STEP_GROUP;
+#pragma unroll
+            for (int d = 0; d < kDown; ++d)
+#pragma unroll
+                for (int a = 0; a < kAcross; ++a) scale[16 * d * scales_stride + a] = uint8_t(byte[d][a]);
+        } else {
+            T* const at = static_cast<T*>(kept) + i * stride + j;
+#pragma unroll
+            for (int d = 0; d < kDown; ++d)
+#pragma unroll
+                for (int a = 0; a < kAcross; ++a) store_some(at + 16 * d * stride + FSDP_STEP_GROUP * a, 8, z[d][a]);
+        }
+    };
+    keep(p.gate, p.gate_scales, p.gate_stride, p.gate_scales_stride, g);
+    keep(p.up, p.up_scales, p.up_stride, p.up_scales_stride, u);
+    T* const at = static_cast<T*>(p.e.out) + i * p.e.out_stride + j;
+    with_act(p.e.act, [&](auto act) {
+        float out[kDown][kAcross][8];
+#pragma unroll
+        for (int d = 0; d < kDown; ++d)
+#pragma unroll
+            for (int a = 0; a < kAcross; ++a)
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    out[d][a][c] = act_value<sizeof(T) == 4>(g[d][a][c], decltype(act)::value) * u[d][a][c];
+#pragma unroll
+        for (int d = 0; d < kDown; ++d)
+#pragma unroll
+            for (int a = 0; a < kAcross; ++a) store_some(at + 16 * d * p.e.out_stride + FSDP_STEP_GROUP * a, 8, out[d][a]);
+    });
+}
 
 // ------------------------------------------------------------------ forward
 
@@ -176,6 +233,15 @@ struct GatedForward {
         } else {
             finish_pair<T, true>(p, i, j, left, g, u);
         }
+    }
+    template <typename T, int kDown, int kAcross>
+    __device__ static __forceinline__ void put_whole(const PairProduct& p, int64_t i, int64_t j, const float (&g)[kDown][kAcross][8],
+                                                     const float (&u)[kDown][kAcross][8]) {
+        finish_whole<T>(p, i, j, g, u);
+    }
+    // Whether the tile at row i, columns j (of g) on goes to its places whole.
+    __device__ static __forceinline__ bool whole(const PairProduct& p, int64_t i, int64_t j, int tile) {
+        return p.count == 1 && i + tile <= p.m && j + tile / 2 <= p.inner;
     }
     __device__ static __forceinline__ void store_parts(const PairProduct& p, int part, int64_t i, int64_t j, int left, const float (&g)[8],
                                                        const float (&u)[8]) {

@@ -48,6 +48,15 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
     return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xf, 0xf, false)));   // lanes 2 3 0 1
 }
 
+__device__ __forceinline__ i8x8 codes_of(const float (&v)[8], uint32_t byte) {
+    // A factor of 0 makes an infinity a NaN, whose code is no matter: it is 0.
+    const float inverse = scale_inverse(byte == kNotFinite ? 1u : byte);
+    i8x8 q;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) q[c] = byte == kNotFinite ? int8_t(0) : int8_t(int(__builtin_rintf(v[c] * inverse)));
+    return q;
+}
+
 // A lane's eight columns of a group, whose other columns three more lanes hold (group_max): all
 // four are active and call it, those past the row's end with left <= 0.
 template <bool kApart = false>
@@ -58,11 +67,7 @@ __device__ __forceinline__ void save8(const float (&v)[8], int left, int8_t* cod
         if (c < left) most = max(most, __builtin_bit_cast(uint32_t, v[c]) & 0x7fffffffu);
     const uint32_t byte = scale_byte(group_max<kApart>(most));
     if (left <= 0) return;
-    // A factor of 0 makes an infinity a NaN, whose code is no matter: it is 0.
-    const float inverse = scale_inverse(byte == kNotFinite ? 1u : byte);
-    i8x8 q;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) q[c] = byte == kNotFinite ? int8_t(0) : int8_t(int(__builtin_rintf(v[c] * inverse)));
+    const i8x8 q = codes_of(v, byte);
     if (left >= 8) {
         reinterpret_cast<AnyCodes*>(codes)->v = q;
     } else {
