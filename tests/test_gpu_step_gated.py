@@ -362,6 +362,26 @@ def test_8_bits_as_their_values():
         assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+@pytest.mark.parametrize("m,n,k", [(4101, 2052, 520), (1976, 2186, 328)])
+def test_rows_that_are_not_finite_stay_alone(m, n, k):
+    """In tiles that lie in out whole and in those at its edges."""
+    x, gw, uw = (normal(s, *shape).cuda() for s, shape in ((1, (m, k)), (2, (n, k)), (3, (n, k))))
+    bad = [0, 17, 1000, m - 1]
+    poisoned = x.clone()
+    poisoned[bad, 5] = torch.tensor([float("inf"), float("nan"), -float("inf"), float("nan")], dtype=x.dtype, device="cuda")
+    results = []
+    for v in (x, poisoned):
+        out, gate, up = torch.empty(m, n, dtype=x.dtype, device="cuda"), Checkpoint.empty(m, n), Checkpoint.empty(m, n)
+        gated_linear(v, gw, uw, out, gate=gate, up=up)
+        results.append((out, *gate, *up))
+    good = torch.ones(m, dtype=torch.bool)
+    good[bad] = False
+    for clean, other in zip(*results):
+        assert torch.equal(clean[good.cuda()], other[good.cuda()])
+    for codes, scales in (results[1][1:3], results[1][3:5]):
+        assert bool((scales[bad] == 255).all()) and bool((codes[bad] == 0).all())
+
+
 def test_long_sums_in_fp32():
     """Sums over many terms go in runs of 512.  Of random terms the sum of i is sqrt(i / n) of that
     of n, and each addition off by at most 2^-24 of it: all additions of a run by 2^-24 sqrt(512 / 2),
