@@ -186,6 +186,12 @@ fsdp_status fsdp_step_linear_grad(const fsdp_step_linear_grad_args* args, void* 
  * gradient of 0.  Masked logits may be -inf or any finite value; a row whose logits
  * are all -inf has no distribution: NaN.  An advantage of 0 adds nothing, whatever
  * r is.  Differences of logarithms are formed in 64 bits.
+ *
+ * A saved lse is an fp32 value, and below 2^14 the gradient from it takes it as it is:
+ * q and r are off by exp of its rounding, 2^-24 |lse|, at most 2^-11 of themselves.
+ * From 2^14 on (a small tau, a row far from 0 or all at a mask's finite value) that
+ * gradient takes the row's own maximum and sum instead, and is as exact as the one of
+ * fsdp_step_policy.
  */
 typedef struct fsdp_step_policy_args {
     int64_t tokens;                /* >= 0 */
@@ -212,7 +218,7 @@ typedef struct fsdp_step_policy_args {
 
 /* The loss, logp, lse, and with dlogits the gradient in the same pass.  One kernel. */
 fsdp_status fsdp_step_policy(const fsdp_step_policy_args* args, hipStream_t stream);
-/* The gradient from the lse that fsdp_step_policy wrote (loss and logp are not used).  One kernel. */
+/* The gradient from the lse that fsdp_step_policy wrote for these logits (loss and logp are not used).  One kernel. */
 fsdp_status fsdp_step_policy_grad(const fsdp_step_policy_args* args, hipStream_t stream);
 
 #ifdef __cplusplus

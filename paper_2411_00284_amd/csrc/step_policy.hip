@@ -63,6 +63,12 @@ __device__ __forceinline__ void token_loss(const PolicyArgs& a, int64_t row, dou
     }
 }
 
+// A saved lse is rounded to 32 bits, and q and the ratio are off by exp of its rounding: by 2^-11 of
+// themselves below 2^14. From there on (small temperatures, rows far from 0 or all at a mask's finite
+// value) the row's maximum and sum are taken again, which costs another pass over the row: 77 us instead of
+// 66 at 1531 x 50257 in fp16.
+constexpr float kSavedLse = 16384.f;
+
 // kHeld units per thread stay in registers, the others are streamed kStream at a time.
 constexpr int kStream = 4;
 template <typename T, int kThreads, int kHeld>
@@ -93,16 +99,17 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
             continue;
         }
         const float picked = float(s[action]);                  // before an in-place gradient overwrites it
-        const bool gradient = a.dlogits && a.dloss[row] != 0.f;
+        const bool gradient = a.dlogits && a.dloss[row] != 0.f, whole = !a.lse_in || gradient;
+        const bool saved = a.lse_in && fabsf(a.lse_in[row]) < kSavedLse;   // not a NaN
         Unit<T> held[kHeld / 2][2];
         float lone = -INFINITY;
         Softmax x;
-        if (!a.lse_in || gradient) {
+        if (whole) {
 #pragma unroll
             for (int u = 0; u < kHeld; ++u) held[u / 2][u % 2].load(s, t + u * kThreads, units);
             lone = single < vocab ? float(s[single]) : -INFINITY;
         }
-        if (!a.lse_in) {
+        if (whole && !saved) {
 #pragma unroll
             for (int u = 0; u < kHeld / 2; ++u) add_units(x, held[u], c);
             for (int j = t + kHeld * kThreads; j < units; j += kStream * kThreads) {
@@ -126,9 +133,9 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
             x.s = wave_sum(lane < kWaves ? Softmax::moved(ws[lane], mine, Softmax::base(x.m), c) : 0.f);
         }
         if (wave == 0) {                                        // every lane the same
-            const double log_sum = a.lse_in ? 0.0 : log2_of(x.s) * ln2;
+            const double log_sum = saved ? 0.0 : log2_of(x.s) * ln2;
             // The difference to the maximum first: a row of one mask value would lose the sum beside it.
-            const double logp = a.lse_in ? double(picked) * per_tau - double(a.lse_in[row]) : (double(picked) - double(x.m)) * per_tau - log_sum;
+            const double logp = saved ? double(picked) * per_tau - double(a.lse_in[row]) : (double(picked) - double(x.m)) * per_tau - log_sum;
             float loss, slope;
             token_loss(a, row, logp, loss, slope);
             const float weight = gradient ? float(double(a.dloss[row]) * double(slope) * per_tau) : 0.f;
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 4 ? 4 : 5) void policy_kernel(con
             // q = 2^((s - base) c) times what its base leaves: the sum over the row's maximum, or
             // of a saved lse what float(lse tau) misses of it.
             float base = Softmax::base(x.m), factor = -weight / x.s;
-            if (a.lse_in) {
+            if (saved) {
                 const double b = double(a.lse_in[row]) * double(a.tau);
                 base = b > FLT_MAX ? FLT_MAX : b < -FLT_MAX ? -FLT_MAX : float(b);
                 factor = -weight * exp2_fast(float((double(base) - b) * double(c)));

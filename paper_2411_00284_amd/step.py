@@ -127,7 +127,10 @@ def policy_loss_backward(dloss: torch.Tensor, logits: torch.Tensor, actions: tor
                          advantages: torch.Tensor, lse: torch.Tensor, dlogits: torch.Tensor, *, ref_logp=None, clip_low: float = 0.2,
                          clip_high: float = 0.2, kl_weight: float = 0.0, temperature: float = 1.0, stream=None) -> None:
     """The gradient of ``policy_loss`` with respect to the logits, from the
-    ``lse`` it wrote and the gradient ``dloss`` [tokens] of the losses.
-    ``dlogits`` may be ``logits``."""
+    ``lse`` it wrote for them and the gradient ``dloss`` [tokens] of the losses.
+    ``dlogits`` may be ``logits``.  An ``lse`` is rounded to 32 bits: up to a
+    size of 2^14 the probabilities and the ratio share what that leaves of them
+    (2^-24 of its size); of larger ones, as a small temperature or a row at a
+    mask's value has them, the row's own is formed again."""
     _check(_lib().policy(True, logits, actions, old_logp, advantages, ref_logp, dloss, None, None, lse, dlogits, clip_low, clip_high,
                          kl_weight, temperature, stream), "fsdp_step_policy_grad")
