@@ -21,9 +21,16 @@
  * byte 255 and stands for NaN.  So codes [rows, cols] are int8 and scales
  * [rows, ceil(cols / 32)] uint8, each with a row stride of its own.  The scale is
  * a power of two because what a group stands for is then exact in bf16, fp16 and
- * fp32 (beyond their range apart: fp16 values above 65504 become infinite): the
- * matrix cores take it with no further rounding.  A step is at most 2^-6 of the
- * group's largest magnitude, a value is off by half of one.
+ * fp32, between the ends of their ranges: the matrix cores take it with no further
+ * rounding.  A step is at most 2^-6 of the group's largest magnitude, a value is off by
+ * half of one.
+ *
+ * At the ends: what passes a type's range is infinite in it, and the largest values of a
+ * group may round up to a power of two past it (M from 65280 on stands for 65536, infinite
+ * in fp16; from 255 * 2^120 on for 2^128, infinite in every type).  A group with steps
+ * below 2^-24, of M below 2^-18, is rounded a second time where it is read as fp16, to
+ * multiples of 2^-24, unless it was saved from fp16.  (fsdp_step_gated saves its sums in
+ * 32 bits.)
  */
 #ifndef FSDP_STEP_H
 #define FSDP_STEP_H

@@ -47,8 +47,11 @@ class Checkpoint(NamedTuple):
     127), one for each 32 neighbouring columns of a row.  A scale is the least
     with which its largest value rounds to 127 or less; codes are rounded to
     nearest even.  A group that holds a value that is not finite stands for NaN
-    (scale 255).  What it stands for is exact in every type, fp16 above 65504
-    apart.  Both tensors may have any row stride."""
+    (scale 255).  What it stands for is exact in every type between the ends
+    of its range: from 65280 on in fp16, and from 255 * 2^120 on in all, the
+    largest of a group may become infinite; groups below 2^-18 that were not
+    saved from fp16 are rounded to multiples of 2^-24 where they are read as
+    fp16.  Both tensors may have any row stride."""
     codes: torch.Tensor
     scales: torch.Tensor
 
