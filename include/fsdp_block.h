@@ -140,7 +140,7 @@ fsdp_status fsdp_block_norm_grad(const fsdp_norm_grad_args* args, void* workspac
  * its argument more in its tail), by up to 7e-6 before the rounding to 16 bits; what
  * takes an exponential below 2^-126 is 0.
  *
- * Sizes are at most 2^30, with 2^22 tiles of 64 x 64 in every matrix.  With more than
+ * Sizes are below 2^30, with 2^22 tiles of 64 x 64 in every matrix.  With more than
  * four rows of x, 64 rows of x and of weight (fp32: 64 and 128; all, if there are fewer)
  * must lie within 2^31 bytes, at rows of k in whole 128-byte lines: k up to 17 million in
  * 16 bits, 4.2 million in fp32.  The gradient's products ask the same of n for dz, and of k

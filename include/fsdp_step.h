@@ -78,9 +78,10 @@ fsdp_status fsdp_step_restore(const fsdp_step_restore_args* args, hipStream_t st
  * the type, or in 8 bits where their scales are given.  out, and the 8 bits, are
  * computed from g and u before these are rounded.
  *
- * Sizes are at most 2^29, with 2^22 tiles of 64 x 64 in every matrix, both weights
- * counted as one of 2 n rows.  With more than four rows of x, 64 rows of x and 128 of a
- * weight must lie within 2^31 bytes, at rows of k in whole 128-byte lines.  Else
+ * Sizes are below 2^29, with 2^22 tiles of 64 x 64 in every matrix, both weights
+ * counted as one of 2 n rows.  64 rows of x and 128 of a weight must lie within 2^31
+ * bytes, at rows of k in whole 128-byte lines, but for up to four rows of x, which go
+ * without tiles where n is below 2^26 and nothing is kept in 8 bits.  Else
  * FSDP_ERR_OVERFLOW.
  */
 typedef struct fsdp_step_gated_args {
@@ -100,9 +101,9 @@ typedef struct fsdp_step_gated_args {
 } fsdp_step_gated_args;
 
 fsdp_status fsdp_step_gated_workspace(const fsdp_step_gated_args* args, int64_t* bytes);
-/* One kernel; one before it where x or a weight lies off the 16-byte grid (up to
- * four rows of x excepted), one after it where few tiles split the sum over k,
- * or many leave a last round of few.  None where out has no elements. */
+/* One kernel; for tiles one before it where x or a weight lies off the 16-byte grid, and
+ * one after it where few tiles split the sum over k, or many leave a last round of
+ * few.  None where out has no elements. */
 fsdp_status fsdp_step_gated(const fsdp_step_gated_args* args, void* workspace, int64_t workspace_bytes,
                             hipStream_t stream);
 

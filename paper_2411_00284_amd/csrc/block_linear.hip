@@ -226,7 +226,7 @@ fsdp_status check_sizes(int64_t m, int64_t n, int64_t k, fsdp_dtype dtype, fsdp_
     if (!known_dtype(dtype)) return fail(FSDP_ERR_INVALID, "unknown dtype");
     if (act < FSDP_ACT_NONE || act > FSDP_ACT_GELU_TANH) return fail(FSDP_ERR_INVALID, "unknown activation");
     // Row and column counts travel as 32-bit values in the kernels, tiles as a launch's workgroups.
-    if (m > INT32_MAX / 2 || n > INT32_MAX / 2 || k > INT32_MAX / 2) return fail(FSDP_ERR_OVERFLOW, "a size is above 2^30");
+    if (m > INT32_MAX / 2 || n > INT32_MAX / 2 || k > INT32_MAX / 2) return fail(FSDP_ERR_OVERFLOW, "a size is 2^30 or more");
     const int64_t most = int64_t(1) << 22;
     if (ceil_div(m, 64) * ceil_div(n, 64) > most || ceil_div(m, 64) * ceil_div(k, 64) > most ||
         ceil_div(n, 64) * ceil_div(k, 64) > most)

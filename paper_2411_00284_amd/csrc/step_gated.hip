@@ -339,7 +339,7 @@ fsdp_status check_sizes(int64_t m, int64_t n, int64_t both, int64_t k, fsdp_dtyp
     if (!known_dtype(dtype)) return fail(FSDP_ERR_INVALID, "unknown dtype");
     if (act < FSDP_ACT_NONE || act > FSDP_ACT_GELU_TANH) return fail(FSDP_ERR_INVALID, "unknown activation");
     const int64_t size = INT32_MAX / 2 / both;
-    if (m > size || n > size || k > size) return fail(FSDP_ERR_OVERFLOW, "a size is above 2^%d", both == 2 ? 29 : 30);
+    if (m > size || n > size || k > size) return fail(FSDP_ERR_OVERFLOW, "a size is 2^%d or more", both == 2 ? 29 : 30);
     // Of dz with each part in whole lines.
     const int64_t most = int64_t(1) << 22, wide = both * ceil_div(n, 64);
     if (ceil_div(m, 64) * wide > most || ceil_div(m, 64) * ceil_div(k, 64) > most || wide * ceil_div(k, 64) > most)
