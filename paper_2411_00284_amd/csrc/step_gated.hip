@@ -258,7 +258,10 @@ constexpr Form kRings[] = {
 // fp32, from products of 2048 x 1024 x 688 to 5000 x 2500 x 1500. A gradient's small tiles are those
 // of 64 x 64, two on a CU: the weights' gradients of 2048 x 688 -> 1024 take 67 us instead of 74 in
 // tiles of 64 x 128, of 59 x 28672 -> 256 the whole call 114 instead of 164. A linear layer's gradient
-// has the forms that it has without 8 bits, and so its bits.
+// has the forms and the parts of k that it has without 8 bits: where no part is longer than a run
+// (step_product.h), 512 k, its bits too. Longer ones are summed in runs here and one term after the other
+// there: 4096 x 1024 -> 4096 is 4.1e-7 off 64 bits (2-norm) from an x in 8 bits, in 561 us, and 1.14e-6
+// from its values, in 497.
 constexpr Form kForwards32[] = {{128, 128, 2, 2, 2.10, 4.15, 5.0}, {64, 128, 4, 1, 1.22, 1.28, 4.0}};
 constexpr Form kGrads32[] = {{128, 128, 2, 2, 2.10, 4.15, 5.0}, {64, 64, 4, 2, 0.58, 1.14, 3.5}};
 constexpr Forms kForward16{kRings, 4, kRings + 1, 1}, kGrad16{kRings, 5, kRings + 1, 1};
