@@ -43,8 +43,6 @@ void* kept_matrix(Call& c, const Kept& k, const char* name, int64_t rows, int64_
     return c.matrix(k.values, name, rows, cols, stride);
 }
 
-// The codes' pointer may be NULL for a matrix without elements: its scales' too.
-
 // save(x, codes_and_scales, stream)
 PyObject* save(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return entry(n, 3, [&]() -> fsdp_status {

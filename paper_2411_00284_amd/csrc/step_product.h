@@ -25,6 +25,10 @@ struct PairProduct : Product {
     int64_t out2_stride;
 };
 
+// fp32: runs of 512 k. One sum over k = 7864 is off by 1.6e-6 of the result (2-norm), in runs by
+// 4.1e-7; they cost 1 to 3 % (1910 x 1024 x 7864: 551 us, 537 without).
+constexpr int kRunSteps = 16;
+
 // Columns of g (or u) in a row of the parts.
 __device__ __host__ __forceinline__ int64_t part_columns(int64_t inner) { return (inner + 7) / 8 * 8; }
 
@@ -65,9 +69,6 @@ __device__ __forceinline__ void finish_pair(const PairProduct& p, int64_t i, int
     store_some(static_cast<T*>(p.e.out) + i * p.e.out_stride + j, left, out);
 }
 
-// fp32: runs of 512 k. One sum over k = 7864 is off by 1.6e-6 of the result (2-norm), in runs by
-// 4.1e-7; they cost 1 to 3 % (1910 x 1024 x 7864: 551 us, 537 without).
-constexpr int kRunSteps = 16;
 // As finish_pair, kApart, of several times eight columns that all exist: kDown rows 16 apart of kAcross
 // groups. Without branches of their own, so that their chains of instructions overlap where a SIMD
 // has one wave.
@@ -383,7 +384,7 @@ struct Plain : OneMatrix {
             // A piece that lies in one output whole: rows together, without branches of their own (the
             // gradient of 1024 x 14336 x 1024 in fp16: 171 us instead of 178).
             if (p.count == 1 && first_j + kWide <= p.n && Kind::whole(p, first_i + first, rows)) {
-                constexpr int kMany = kWide >= 64 ? 4 : 2;
+                constexpr int kMany = 4;
                 const RowsOut to = Kind::template out<T>(p, first_i + first);
                 T* const at = static_cast<T*>(to.p) + lane / kLanes * to.stride + j;
 #pragma unroll 1
