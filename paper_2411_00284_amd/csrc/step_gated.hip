@@ -435,7 +435,7 @@ struct Grad {
     int act = 0;
     bool two = false, dx = false, dweight = false, saved_x = false;
     bool as_is = false;              // dz is dout itself
-    Source weight[2], x, dout;
+    Source weight[2] = {}, x = {}, dout = {};
     Shape dx_shape, dw_shape;
     Cut dx_cut, dw_cut;
     int64_t part_rows = 1, row_parts = 0;
