@@ -193,7 +193,8 @@ fsdp_status fsdp_step_linear_grad(const fsdp_step_linear_grad_args* args, void* 
  * other values are; one with a of vocab or more NaN.  A dloss of 0 gives a
  * gradient of 0.  Masked logits may be -inf or any finite value; a row whose logits
  * are all -inf has no distribution: NaN.  An advantage of 0 adds nothing, whatever
- * r is.  Differences of logarithms are formed in 64 bits.
+ * r is.  Differences of logarithms are formed in 64 bits, and dloss * slope / tau is then
+ * an fp32 value: a row in which it passes their range has a gradient that is not finite.
  *
  * A saved lse is an fp32 value, and below 2^14 the gradient from it takes it as it is:
  * q and r are off by exp of its rounding, 2^-24 |lse|, at most 2^-11 of themselves.

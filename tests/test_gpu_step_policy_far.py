@@ -85,3 +85,21 @@ def test_rows_far_from_zero(dtype, vocab):
     now = torch.log_softmax(d, 1).gather(1, actions[:, None])[:, 0].float()
     made[2], made[4] = now + torch.tensor([0.1, -0.1, 0.05, 0.3, -0.3, 0.1, 0.0]), now + 0.2
     assert check(made, options(), (dtype, vocab)).tolist() == [True, True, False, True, True, False, False]
+
+
+@pytest.mark.parametrize("tokens,vocab", [(300, 2003), (300, 6001), (9, 20011), (300, 20011)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_bits_of_the_one_pass(dtype, tokens, vocab):
+    """In every form of the kernel that both calls take: the row's own sums are the first call's, and so are all bits."""
+    print("far forms", dtype, tokens, vocab, flush=True)
+    logits, actions, old, adv, ref, dloss = make(131, tokens, vocab, DTYPES[dtype])
+    logits[::3] += 3e4
+    actions[::5], dloss[1::7] = -1, 0.0
+    g, more = [v.cuda() for v in (logits, actions, old, adv)], dict(options(), ref_logp=ref.cuda(), dloss=dloss.cuda())
+    lse, first, back = torch.empty(tokens, device="cuda"), torch.empty_like(g[0]), torch.full_like(g[0], float("nan"))
+    policy_loss(*g, lse=lse, dlogits=first, **more)
+    policy_loss_backward(more.pop("dloss"), *g, lse, back, **more)
+    far = lse.abs() >= KEPT
+    assert bool(far.any()) and not bool(far.all()) and torch.equal(first[far], back[far])
+    masked = g[1] < 0
+    assert not bool(back[masked].any()) and not bool(back[1::7].any()) and bool(back[far].any())
